@@ -33,6 +33,10 @@ EXPORTED_SYMBOLS = [
     "ltri_get_rep_keys", "ltri_get_selection", "ltri_get_token_list", "ltri_get_index_tokens", "ltri_get_theta",
     "ltri_strerror",
     "ltri_last_error", "ltri_version",
+    # include/ltri_paged.h
+    "ltri_paged_workspace_bytes", "ltri_paged_create", "ltri_paged_create_dry", "ltri_paged_destroy",
+    "ltri_paged_set_stream", "ltri_paged_append", "ltri_paged_attend", "ltri_paged_step", "ltri_paged_evict",
+    "ltri_paged_sync_status", "ltri_paged_last_error",
     # include/ltri_bench.h: measurement helpers, not part of the product boundary
     "ltri_measure_mfma_peak", "ltri_measure_copy_peak", "ltri_measure_read_peak",
 ]
@@ -55,6 +59,15 @@ class LtriConfig(C.Structure):
         ("lam", C.c_float), ("index_min", C.c_int32), ("index_max", C.c_int32), ("ratio_mode", C.c_int32),
         ("theta_quantile", C.c_float), ("unit_tokens", C.c_int32), ("kv_offload", C.c_int32),
         ("index_block_max", C.c_int32),
+    ]
+
+
+class LtriPagedConfig(C.Structure):
+    _fields_ = [
+        ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+        ("page_tokens", C.c_int32), ("n_pages", C.c_int32), ("table_pages", C.c_int32), ("max_seqs", C.c_int32),
+        ("rows_max", C.c_int32), ("weights", C.c_int32),
+        ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64),
     ]
 
 
@@ -104,6 +117,16 @@ def load_library() -> C.CDLL:
         "ltri_get_token_list": [vp, i32, i32, i32, pi32, i32, pi32],
         "ltri_get_index_tokens": [vp, i32, i32, i32, C.POINTER(C.c_uint32), i32],
         "ltri_get_theta": [vp, i32, i32, i32, C.POINTER(C.c_double)],
+        "ltri_paged_workspace_bytes": [C.POINTER(LtriPagedConfig), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
+        "ltri_paged_create": [C.POINTER(LtriPagedConfig), vp, vp, vp, vp, vp, vp, vp, C.POINTER(vp)],
+        "ltri_paged_create_dry": [C.POINTER(LtriPagedConfig), C.POINTER(vp)],
+        "ltri_paged_destroy": [vp],
+        "ltri_paged_set_stream": [vp, vp],
+        "ltri_paged_append": [vp, i32, vp, vp, vp, vp, vp, vp, i32],
+        "ltri_paged_attend": [vp, i32, vp, vp, vp, i32, vp, vp, C.c_float],
+        "ltri_paged_step": [vp, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, C.c_float],
+        "ltri_paged_evict": [vp, i32, vp, vp, vp, i32, i32, i32],
+        "ltri_paged_sync_status": [vp],
         "ltri_measure_mfma_peak": [vp, C.c_size_t, i32, vp, C.POINTER(C.c_double)],
         "ltri_measure_copy_peak": [vp, vp, C.c_size_t, vp, C.POINTER(C.c_double)],
         "ltri_measure_read_peak": [vp, C.c_size_t, vp, C.c_size_t, vp, C.POINTER(C.c_double)],
@@ -116,6 +139,8 @@ def load_library() -> C.CDLL:
     lib.ltri_strerror.restype = C.c_char_p
     lib.ltri_last_error.argtypes = [vp]
     lib.ltri_last_error.restype = C.c_char_p
+    lib.ltri_paged_last_error.argtypes = [vp]
+    lib.ltri_paged_last_error.restype = C.c_char_p
     lib.ltri_version.argtypes = []
     lib.ltri_version.restype = C.c_char_p
     _LIB = lib

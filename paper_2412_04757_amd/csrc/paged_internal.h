@@ -1,0 +1,80 @@
+// Declarations shared by the host side and the kernels of the paged cache (ltri_paged.h).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+#include "ltri_paged.h"
+
+namespace ltri {
+
+constexpr int PAGED_TILE = 32;             // tokens per attention tile; rows of scores are padded to it
+
+struct PagedDims {
+  int Hq, Hkv, G, d, dtype, elt;
+  int page_shift, n_pages, table_pages, max_seqs, rows_max, weights;
+  long long page_stride, head_stride, token_stride;    // elements
+  long long cap_tokens;                                // table_pages * page_tokens
+  long long score_tiles;                               // tiles of scores, and of lists of moves, the scratch has room for
+};
+
+// Byte offsets in the caller's buffers.
+struct PagedLayout {
+  size_t err;          // int32 [4]
+  size_t tickets;      // int32 [max_seqs * Hkv]  zero between launches
+  size_t state_total;
+  size_t lse;          // float [max_seqs][rows_max][Hq]  log-sum-exp, log2 domain
+  size_t scores;       // float [score_tiles][Hkv][rows_max * G][PAGED_TILE]   (a sequence's tiles together, see score_base)
+  size_t move_head;    // int64 [max_seqs * Hkv][2]  offset of a list of moves and its length
+  size_t moves;        // int32 [score_tiles][Hkv][PAGED_TILE]
+  size_t scratch_total;
+};
+
+struct PagedCall {
+  PagedDims D;
+  char* k; char* v; float* weight; int32_t* pos;
+  int32_t* err; int32_t* tickets;
+  float* lse2; float* scores; long long* move_head; int32_t* moves;
+  const int32_t* table; int32_t* lens; const int32_t* seen;
+  int seq_count;
+  // append, step
+  const void* k_new; const void* v_new; const float* w_new;
+  // append, attend, step: new rows
+  int n;
+  const void* q; void* out; float* lse; float decay;
+  // evict
+  int keep, n_sink, n_recent;
+};
+
+hipError_t launch_paged_append(const PagedCall& a, hipStream_t s);
+hipError_t launch_paged_attend(const PagedCall& a, hipStream_t s);      // k_new != NULL: the rows are written, too
+hipError_t launch_paged_evict(const PagedCall& a, hipStream_t s);
+hipError_t launch_fill_zero(void* p, size_t bytes, hipStream_t s);      // seg.hip
+
+#if defined(__HIPCC__)
+// Length of a sequence; one that the table cannot hold is reported and taken as empty.
+__device__ __forceinline__ int paged_len(const PagedCall& a, int s) {
+  const int n = a.lens[s];
+  if (n > a.D.cap_tokens) {
+    atomicCAS(a.err, 0, LTRI_ECAPACITY);
+    return 0;
+  }
+  return n > 0 ? n : 0;
+}
+// Page of the token at place i of a sequence, or -1 (reported) if the table names none in the pool.
+__device__ __forceinline__ int paged_page(const PagedCall& a, int s, int i) {
+  const int p = a.table[(size_t)s * a.D.table_pages + (i >> a.D.page_shift)];
+  if ((unsigned)p < (unsigned)a.D.n_pages) return p;
+  atomicCAS(a.err, 0, LTRI_EINVAL);
+  return -1;
+}
+// Element offset of a token's row in the pools, and its index in weight and pos.
+__device__ __forceinline__ long long paged_row(const PagedDims& D, int page, int h, int i) {
+  return page * D.page_stride + h * D.head_stride + (i & ((1 << D.page_shift) - 1)) * D.token_stride;
+}
+__device__ __forceinline__ size_t paged_mark(const PagedDims& D, int page, int h, int i) {
+  return (((size_t)page * D.Hkv + h) << D.page_shift) + (i & ((1 << D.page_shift) - 1));
+}
+__device__ __forceinline__ int paged_tiles(int len) { return (len + PAGED_TILE - 1) / PAGED_TILE; }
+#endif
+
+}  // namespace ltri

@@ -1,0 +1,186 @@
+"""The paged cache without a GPU: sizes, refusals (dry handles), and the oracle against dense attention."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as O
+from paper_2412_04757_amd import LtriError, LtriPagedCache, load_library, paged_config
+
+EINVAL, ECAPACITY = -1, -3
+
+
+def config(**kw):
+    a = dict(n_q_heads=8, n_kv_heads=2, head_dim=64, dtype="bf16", page_tokens=16, n_pages=12, table_pages=4, max_seqs=3, rows_max=4,
+             weights=True)
+    a.update(kw)
+    return paged_config(**a)
+
+
+def sizes(cfg):
+    sb, cb = C.c_size_t(), C.c_size_t()
+    return load_library().ltri_paged_workspace_bytes(C.byref(cfg), C.byref(sb), C.byref(cb)), sb.value, cb.value
+
+
+@pytest.mark.parametrize("kw", [
+    dict(n_q_heads=7), dict(n_q_heads=0), dict(n_kv_heads=0), dict(n_q_heads=258, n_kv_heads=2), dict(head_dim=96), dict(head_dim=256),
+    dict(page_tokens=0), dict(page_tokens=24), dict(page_tokens=8192), dict(n_pages=0), dict(table_pages=0),
+    dict(table_pages=1 << 27), dict(max_seqs=0), dict(max_seqs=4097), dict(rows_max=0), dict(rows_max=65),
+    dict(page_stride=2048, head_stride=1024, token_stride=60),            # rows overlap
+    dict(page_stride=2048, head_stride=1024, token_stride=68),            # not a multiple of 16 bytes
+    dict(page_stride=2048, head_stride=512, token_stride=64),             # heads overlap
+    dict(page_stride=1024, head_stride=1024, token_stride=64),            # pages overlap
+    dict(page_stride=-2048, head_stride=1024, token_stride=64),
+])
+def test_unsupported_configurations_are_refused(kw):
+    assert sizes(config(**kw))[0] == EINVAL
+    with pytest.raises(LtriError) as e:
+        LtriPagedCache(config(**kw), None, dry=True)
+    assert e.value.status == EINVAL
+
+
+def test_null_configuration_and_pointers():
+    lib = load_library()
+    assert lib.ltri_paged_workspace_bytes(None, None, None) == EINVAL
+    h = C.c_void_p()
+    cfg = config()
+    assert lib.ltri_paged_create_dry(C.byref(cfg), None) == EINVAL
+    assert lib.ltri_paged_create(C.byref(cfg), None, None, None, None, None, None, None, C.byref(h)) == EINVAL and not h
+    for f, n in (("destroy", 0), ("sync_status", 0)):
+        assert getattr(lib, "ltri_paged_" + f)(None) == EINVAL
+    assert lib.ltri_paged_append(None, 1, None, None, None, None, None, None, 1) == EINVAL
+    assert lib.ltri_paged_attend(None, 1, None, None, None, 1, None, None, -1.0) == EINVAL
+    assert lib.ltri_paged_step(None, 1, None, None, None, None, None, None, 1, None, None, -1.0) == EINVAL
+    assert lib.ltri_paged_evict(None, 1, None, None, None, 1, 0, 0) == EINVAL
+    assert lib.ltri_paged_last_error(None) == b""
+
+
+def test_sizes_and_strides():
+    ok, state, scratch = sizes(config())
+    assert ok == 0 and state % 256 == 0 and scratch % 256 == 0 and scratch > 0
+    assert sizes(config(weights=False))[2] < scratch                       # no scores, no lists
+    assert sizes(config(n_pages=1000, table_pages=400))[2] > scratch       # they grow with the pool,
+    assert sizes(config(n_pages=1 << 30))[2] < 2 * scratch                 # but not beyond what the tables can name
+    # [page][token][head][d], and keys and values side by side in one pool
+    assert sizes(config(page_stride=2048, head_stride=64, token_stride=128))[0] == 0
+    assert sizes(config(page_stride=4096, head_stride=1024, token_stride=64))[0] == 0
+    # an axis of one entry may have any stride
+    assert sizes(config(n_kv_heads=1, page_stride=1024, head_stride=7, token_stride=64))[0] == 0
+    assert sizes(config(page_tokens=1, page_stride=128, head_stride=64, token_stride=3))[0] == 0
+
+
+class Address:
+    def __init__(self, p):
+        self.p = p
+
+    def data_ptr(self):
+        return self.p
+
+
+def call(cache, name, **kw):
+    """A call with good arguments but those given."""
+    lib, h = cache.lib, cache.handle
+    a = dict(n=2, table=256, lens=256, seen=256, k=256, v=256, w=256, rows=1, q=256, out=256, lse=256, decay=1.0, keep=20, sink=4, recent=8)
+    a.update(kw)
+    if name == "append":
+        return lib.ltri_paged_append(h, a["n"], a["table"], a["lens"], a["seen"], a["k"], a["v"], a["w"], a["rows"])
+    if name == "attend":
+        return lib.ltri_paged_attend(h, a["n"], a["table"], a["lens"], a["q"], a["rows"], a["out"], a["lse"], a["decay"])
+    if name == "step":
+        return lib.ltri_paged_step(h, a["n"], a["table"], a["lens"], a["seen"], a["k"], a["v"], a["q"], a["rows"], a["out"], a["lse"], a["decay"])
+    return lib.ltri_paged_evict(h, a["n"], a["table"], a["lens"], a["seen"], a["keep"], a["sink"], a["recent"])
+
+
+EVERY = ("append", "attend", "step", "evict")
+
+
+@pytest.mark.parametrize("names,kw,status", [
+    (EVERY, dict(), 0), (EVERY, dict(n=0), EINVAL), (EVERY, dict(n=4), EINVAL), (EVERY, dict(table=None), EINVAL), (EVERY, dict(lens=None), EINVAL),
+    (EVERY, dict(lens=258), EINVAL), (EVERY, dict(table=257), EINVAL),
+    (("append", "step", "evict"), dict(seen=None), EINVAL), (("append", "step"), dict(k=None), EINVAL), (("append", "step"), dict(v=None), EINVAL),
+    (("append", "step"), dict(k=264), EINVAL), (("append", "step"), dict(v=258), EINVAL), (("append", "step"), dict(rows=0), EINVAL),
+    (("append",), dict(rows=64), 0), (("append",), dict(rows=65), ECAPACITY), (("append",), dict(w=None), 0), (("append",), dict(w=257), EINVAL),
+    (("attend", "step"), dict(rows=5), EINVAL), (("attend", "step"), dict(rows=4), 0), (("attend",), dict(rows=0), EINVAL),
+    (("attend", "step"), dict(q=None), EINVAL), (("attend", "step"), dict(out=None), EINVAL), (("attend", "step"), dict(q=272), 0),
+    (("attend", "step"), dict(q=260), EINVAL), (("attend", "step"), dict(out=264), EINVAL), (("attend", "step"), dict(lse=None), 0),
+    (("attend", "step"), dict(lse=258), EINVAL), (("attend", "step"), dict(decay=float("nan")), EINVAL),
+    (("attend", "step"), dict(decay=float("inf")), EINVAL), (("attend", "step"), dict(decay=-1.0), 0), (("attend", "step"), dict(decay=0.0), 0),
+    (("evict",), dict(keep=0), EINVAL), (("evict",), dict(keep=-1), EINVAL), (("evict",), dict(sink=-1), EINVAL),
+    (("evict",), dict(recent=-1), EINVAL), (("evict",), dict(keep=12), 0), (("evict",), dict(keep=11), EINVAL),
+    (("evict",), dict(sink=2147483647, recent=2147483647), EINVAL), (("evict",), dict(keep=2147483647), 0),
+])
+def test_arguments_are_checked(names, kw, status):
+    cache = LtriPagedCache(config(), None, dry=True)
+    for name in names:
+        assert call(cache, name, **kw) == status, (name, cache.lib.ltri_paged_last_error(cache.handle))
+        if status:
+            assert cache.lib.ltri_paged_last_error(cache.handle)
+
+
+def test_a_cache_without_weights():
+    cache = LtriPagedCache(config(weights=False), None, dry=True)
+    assert call(cache, "append", w=None, seen=None) == 0 and call(cache, "append", seen=None) == EINVAL
+    assert call(cache, "attend") == EINVAL and call(cache, "attend", decay=-1.0) == 0
+    assert call(cache, "step", decay=0.0, seen=None) == EINVAL and call(cache, "step", decay=-1.0, seen=None) == 0
+    assert call(cache, "evict") == EINVAL
+    assert cache.sync_status() == 0
+
+
+def test_the_binding_checks_shapes_types_and_density():
+    cache = LtriPagedCache(config(), None, dry=True)
+    t, n = torch.zeros((2, 4), dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    k, q = torch.zeros((2, 2, 3, 64), dtype=torch.bfloat16), torch.zeros((2, 3, 8, 64), dtype=torch.bfloat16)
+    cache.append(t, n, n, k, k)
+    assert cache.attend(t, n, q).shape == q.shape and cache.step(t, n, n, k, k, q).shape == q.shape
+    cache.evict(t, n, n, 20)
+    bad = [lambda: cache.append(t[:, :3], n, n, k, k), lambda: cache.append(t, n[:1], n, k, k), lambda: cache.append(t.long(), n, n, k, k),
+           lambda: cache.append(t, n, n, k, k[:, :, :2]), lambda: cache.append(t, n, n, k.float(), k), lambda: cache.append(t, n, n.float(), k, k),
+           lambda: cache.append(t, n, n, k.transpose(1, 2), k), lambda: cache.append(t, n, n, k, k, w_new=torch.zeros(2, 2, 2)),
+           lambda: cache.attend(t, n, q[:, :, :4]), lambda: cache.attend(t, n, q[:1]), lambda: cache.attend(t, n, q, lse=torch.zeros(2, 3)),
+           lambda: cache.attend(t, n, q, out=q[:, :2]), lambda: cache.attend(t, n, q.float()), lambda: cache.step(t, n, n, k, k, q[:, :2].contiguous()),
+           lambda: cache.attend(t, n, q.transpose(0, 1).contiguous().transpose(0, 1)), lambda: cache.evict(t, n[:1], n, 20)]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
+    with pytest.raises(LtriError):
+        cache.attend(t, n, torch.zeros((2, 5, 8, 64), dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        paged_config(8, 2, 64, "fp16", 16, 12, 4, 3)
+
+
+def test_pools_of_a_wrong_shape_are_refused():
+    good = torch.zeros((12, 2, 16, 64), dtype=torch.bfloat16)
+    for k, v in ((good, None), (good[:11], good[:11]), (good.float(), good.float()), (good.transpose(2, 3), good.transpose(2, 3)),
+                 (good, torch.zeros((12, 16, 2, 64), dtype=torch.bfloat16).transpose(1, 2))):
+        with pytest.raises(ValueError):
+            LtriPagedCache(config(), None, dry=True, k_pages=k, v_pages=v)
+    other = torch.zeros((12, 16, 2, 64), dtype=torch.bfloat16).transpose(1, 2)
+    LtriPagedCache(config(), None, dry=True, k_pages=other, v_pages=other)
+
+
+def test_the_oracle_is_dense_attention():
+    """Pages in order and all tokens visible: softmax(q K^T / sqrt(d)) V by matrices, and the weights add up to rows x group."""
+    rng = np.random.default_rng(1)
+    k, v = rng.normal(size=(2, 4, 2, 8, 16))
+    q = rng.normal(size=(1, 3, 4, 16))
+    weight = np.zeros((4, 2, 8))
+    out, lse = O.attend(k, v, weight, [[0, 1, 2, 3]], [29], q, decay=0.0)
+    K, V = (x.transpose(1, 0, 2, 3).reshape(2, 32, 16)[:, :29] for x in (k, v))
+    for r in range(3):
+        for h in range(4):
+            e = np.exp(K[h // 2][:27 + r] @ q[0, r, h] / 4.0)
+            assert np.allclose(out[0, r, h], e @ V[h // 2][:27 + r] / e.sum()) and np.isclose(lse[0, r, h], np.log(e.sum()))
+    assert np.allclose(weight.sum((0, 2)), 6.0) and (weight.transpose(1, 0, 2).reshape(2, 32)[:, 29:] == 0).all()
+
+
+def test_the_oracle_evicts_the_lightest():
+    rng = np.random.default_rng(2)
+    k, v = rng.normal(size=(2, 3, 1, 4, 2))
+    weight = np.array([[[5.0, 1, 1, 7]], [[0, 1, 9, 2]], [[0, 0, 3, 0]]])
+    pos = np.arange(12).reshape(3, 1, 4)
+    lens, k0 = np.array([12]), k.copy()
+    O.evict(k, v, weight, pos, [[0, 1, 2]], lens, [12], 7, n_sink=0, n_recent=2)
+    # stay: 10 and 11 (the latest), 6, 3, 0 and 7 by weight, and of the tokens of weight 1 the first
+    assert lens[0] == 7 and list(pos.reshape(-1)[:7]) == [0, 1, 7, 3, 10, 11, 6]
+    assert (k[0, 0, 2] == k0[1, 0, 3]).all() and (k[1, 0, 0] == k0[2, 0, 2]).all() and (k[2] == k0[2]).all()
