@@ -59,7 +59,7 @@ typedef struct {
   int32_t max_seqs;                          /* most sequences in one call                 */
   int32_t rows_max;                          /* most query rows per sequence in one call   */
   int32_t weights;                           /* 1: weights and positions are kept          */
-  /* Elements from a page, KV head, token to the next, multiples of 16 bytes; keys and values alike. All 0: dense
+  /* Elements from a page, KV head, token to the next (the last at most 2^24), multiples of 16 bytes; keys and values alike. All 0: dense
    * [n_pages][n_kv_heads][page_tokens][head_dim]. Different (page, head, token) must not overlap. */
   int64_t page_stride, head_stride, token_stride;
 } ltri_paged_config;
@@ -86,7 +86,8 @@ int32_t ltri_paged_append(ltri_paged* c, int32_t seq_count, const int32_t* table
 /* q: device [seq_count][n_q][n_q_heads][head_dim], out the same, in the dtype; lse: device fp32
  * [seq_count][n_q][n_q_heads] or NULL (natural-log sum of exponentials of the scaled scores). Row i attends the tokens
  * 0 .. lens - n_q + i, with weights softmax(q.k / sqrt(head_dim)); a row that sees no token, or whose scores are all
- * -infinity, gives 0 and -infinity. Rows of tokens it does not see have no influence, whatever they hold.
+ * -infinity, gives 0 and -infinity. Rows of tokens it does not see have no influence, whatever they hold; an infinity or NaN in
+ * a value row that it does see makes that column infinite or NaN.
  * decay >= 0 (weights = 1 only): every token's weight becomes decay * weight + the sum of its attention weights over
  * the rows and the KV head's query heads; a weight that is not read (decay = 0) may hold anything. decay < 0: weights
  * stay as they are.

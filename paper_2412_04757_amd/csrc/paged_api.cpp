@@ -54,12 +54,13 @@ static int32_t derive(const ltri_paged_config* cfg, PagedDims& D, PagedLayout& L
     D.page_stride = D.Hkv * D.head_stride;
   } else {
     D.page_stride = c.page_stride; D.head_stride = c.head_stride; D.token_stride = c.token_stride;
-    const long long step = 16 / D.elt, most = 1ll << 40;
+    const long long step = 16 / D.elt;
     struct Axis { long long* stride; long long count; } ax[3] = {{&D.page_stride, c.n_pages}, {&D.head_stride, D.Hkv}, {&D.token_stride, c.page_tokens}};
     for (const Axis& x : ax) {
       if (x.count == 1) *x.stride = 0;                  // never stepped over, whatever was given
-      else if (*x.stride < 1 || *x.stride % step || *x.stride > most) return LTRI_EINVAL;
+      else if (*x.stride < 1 || *x.stride % step || *x.stride > 1ll << 40) return LTRI_EINVAL;
     }
+    if (D.token_stride > 1ll << 24) return LTRI_EINVAL;     // 16 tokens lie within 32-bit byte offsets
     // no two rows may overlap: in the order of the strides, each steps over all that the axes below it reach
     for (int i = 0; i < 3; ++i)
       for (int j = i + 1; j < 3; ++j)
@@ -75,7 +76,7 @@ static int32_t derive(const ltri_paged_config* cfg, PagedDims& D, PagedLayout& L
 
   size_t o = 0;
   L.err = o;     o = align_up(o + 16);
-  L.tickets = o; o = align_up(o + (size_t)c.max_seqs * D.Hkv * 4);
+  L.tickets = o; o = align_up(o + (size_t)c.max_seqs * D.Hkv * ((D.rows_max * D.G + 15) / 16) * 4);
   L.state_total = o;
 
   // with weights no page is named twice in a call: its tokens are at most the pool's, and a sequence's last tile is padded
@@ -88,6 +89,8 @@ static int32_t derive(const ltri_paged_config* cfg, PagedDims& D, PagedLayout& L
   if ((double)D.score_tiles * D.Hq * D.rows_max * PAGED_TILE * 4 > 1e15) return LTRI_EINVAL;
   o = 0;
   L.lse = o;    o = align_up(o + (size_t)c.max_seqs * D.rows_max * D.Hq * 4);
+  L.part = o;   o = align_up(o + (size_t)2 * PAGED_MAX_WGS * 16 * D.d * 4);
+  L.part_ml = o; o = align_up(o + (size_t)2 * PAGED_MAX_WGS * 16 * 8);
   L.scores = o; o = align_up(o + (size_t)D.score_tiles * D.Hq * D.rows_max * PAGED_TILE * 4);
   const size_t attend_end = o;
   o = 0;                                                 // the two kinds of call share the scratch
@@ -154,10 +157,11 @@ static int32_t create_impl(const ltri_paged_config* cfg, void* k_pages, void* v_
   b.k = (char*)k_pages; b.v = (char*)v_pages; b.weight = weight; b.pos = pos;
   char* t = (char*)scratch;
   b.err = (int32_t*)(c->state + L.err); b.tickets = (int32_t*)(c->state + L.tickets);
-  b.lse2 = (float*)(t + L.lse); b.scores = (float*)(t + L.scores);
+  b.lse2 = (float*)(t + L.lse); b.part = (float*)(t + L.part); b.part_ml = (unsigned long long*)(t + L.part_ml); b.scores = (float*)(t + L.scores);
   b.move_head = (long long*)(t + L.move_head); b.moves = (int32_t*)(t + L.moves);
   if (!dry) {
     hipError_t e = hipGetDevice(&c->device);
+    if (e == hipSuccess) e = hipDeviceGetAttribute(&b.n_cus, hipDeviceAttributeMultiprocessorCount, c->device);
     if (e == hipSuccess) e = launch_fill_zero(c->state, L.state_total, c->stream);
     if (e != hipSuccess) { delete c; return LTRI_EHIP; }
   }
@@ -259,8 +263,7 @@ int32_t ltri_paged_step(ltri_paged* c, int32_t seq_count, const int32_t* table, 
   if (c->dry) return LTRI_OK;
   OnDevice on(c->device);
   r = check_hip(c, on.e, "device");
-  if (r == LTRI_OK) r = check_hip(c, launch_paged_append(a, c->stream), "append to pages");
-  return r != LTRI_OK ? r : check_hip(c, launch_paged_attend(a, c->stream), "attend over pages");
+  return r != LTRI_OK ? r : check_hip(c, launch_paged_attend(a, c->stream), "step over pages");
 }
 
 int32_t ltri_paged_evict(ltri_paged* c, int32_t seq_count, const int32_t* table, int32_t* lens, const int32_t* seen, int32_t keep,

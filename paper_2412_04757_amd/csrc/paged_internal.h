@@ -7,7 +7,8 @@
 
 namespace ltri {
 
-constexpr int PAGED_TILE = 32;             // tokens per attention tile; rows of scores are padded to it
+constexpr int PAGED_TILE = 32;             // rows of scores are padded to at most this many tokens
+constexpr int PAGED_MAX_WGS = 1024;        // workgroups of an attention launch, at most
 
 struct PagedDims {
   int Hq, Hkv, G, d, dtype, elt;
@@ -20,10 +21,12 @@ struct PagedDims {
 // Byte offsets in the caller's buffers.
 struct PagedLayout {
   size_t err;          // int32 [4]
-  size_t tickets;      // int32 [max_seqs * Hkv]  zero between launches
+  size_t tickets;      // int32 [max_seqs][Hkv][blocks of 16 pairs]  zero between launches
   size_t state_total;
   size_t lse;          // float [max_seqs][rows_max][Hq]  log-sum-exp, log2 domain
-  size_t scores;       // float [score_tiles][Hkv][rows_max * G][PAGED_TILE]   (a sequence's tiles together, see score_base)
+  size_t part;         // float [2 PAGED_MAX_WGS][16][d]  partial results of a workgroup's first and last problem
+  size_t part_ml;      // float2 [2 PAGED_MAX_WGS][16]    their maxima and sums
+  size_t scores;       // float [score_tiles][Hkv][rows_max * G][PAGED_TILE]   (ordered otherwise, see score_rows)
   size_t move_head;    // int64 [max_seqs * Hkv][2]  offset of a list of moves and its length
   size_t moves;        // int32 [score_tiles][Hkv][PAGED_TILE]
   size_t scratch_total;
@@ -33,9 +36,10 @@ struct PagedCall {
   PagedDims D;
   char* k; char* v; float* weight; int32_t* pos;
   int32_t* err; int32_t* tickets;
-  float* lse2; float* scores; long long* move_head; int32_t* moves;
+  float* lse2; float* part; unsigned long long* part_ml; float* scores; long long* move_head; int32_t* moves;
   const int32_t* table; int32_t* lens; const int32_t* seen;
   int seq_count;
+  int n_cus;                 // compute units of the device
   // append, step
   const void* k_new; const void* v_new; const float* w_new;
   // append, attend, step: new rows

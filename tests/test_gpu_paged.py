@@ -422,14 +422,15 @@ def test_captured_steps_follow_lengths_and_tables(gpu_device):
 
 def test_work_goes_to_the_stream_that_is_set(gpu_device):
     c = Case(gpu_device, [900, 20])
-    q = c.on(c.q)
-    torch.cuda.synchronize()
+    there, q = c.on(c.q), torch.zeros(c.q.shape, dtype=torch.bfloat16, device=gpu_device)
+    out, busy = torch.zeros_like(q), torch.randn((4096, 4096), device=gpu_device)
     side = torch.cuda.Stream(gpu_device)
     c.cache.set_stream(side)
-    out = torch.zeros_like(q)
-    gate = torch.cuda.Event()
-    with torch.cuda.stream(side):
-        gate.record()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):                         # the queries come behind other work of that stream
+        for _ in range(20):
+            busy = busy @ busy
+        q.copy_(there)
     c.cache.attend(*c.args(False), q, out=out)
     side.synchronize()
     c.check_attend(out, None, *c.oracle_attend())
