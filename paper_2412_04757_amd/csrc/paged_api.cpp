@@ -77,10 +77,14 @@ static int32_t derive(const ltri_paged_config* cfg, PagedDims& D, PagedLayout& L
   size_t o = 0;
   L.err = o;     o = align_up(o + 16);
   L.tickets = o; o = align_up(o + (size_t)c.max_seqs * D.Hkv * ((D.rows_max * D.G + 15) / 16) * 4);
+  const bool is_long = D.weights && D.cap_tokens > EV_LONG;
+  const size_t slots = (size_t)c.max_seqs * D.Hkv;
+  L.long_state = o; o = align_up(o + (is_long ? slots * EV_LONG_WORDS * 4 : 0));
   L.state_total = o;
 
   // with weights no page is named twice in a call: its tokens are at most the pool's, and a sequence's last tile is padded
   D.score_tiles = 0;
+  D.long_pieces = (int)((D.cap_tokens + EV_CHUNK - 1) / EV_CHUNK + 1);    // (one more: pieces end at the budget)
   if (D.weights) {
     const long long pool = (((long long)c.n_pages << D.page_shift) + PAGED_TILE - 1) / PAGED_TILE + c.max_seqs;
     const long long tables = (D.cap_tokens + PAGED_TILE - 1) / PAGED_TILE * c.max_seqs;
@@ -95,7 +99,12 @@ static int32_t derive(const ltri_paged_config* cfg, PagedDims& D, PagedLayout& L
   const size_t attend_end = o;
   o = 0;                                                 // the two kinds of call share the scratch
   L.move_head = o; o = align_up(o + (D.weights ? (size_t)c.max_seqs * D.Hkv * 16 : 0));
-  L.moves = o;     o = align_up(o + (size_t)D.score_tiles * D.Hkv * PAGED_TILE * 4);
+  const size_t list = (size_t)D.score_tiles * D.Hkv * PAGED_TILE * 4;
+  L.moves = o;     o = align_up(o + list);
+  L.keys = o;      o = align_up(o + (is_long ? list : 0));
+  L.candidates = o; o = align_up(o + (is_long ? list : 0));
+  L.long_slots = o; o = align_up(o + (is_long ? slots * EV_SLOT_BYTES : 0));
+  L.long_counts = o; o = align_up(o + (is_long ? slots * D.long_pieces * 8 : 0));
   L.scratch_total = o > attend_end ? o : attend_end;
   return LTRI_OK;
 }
@@ -159,6 +168,8 @@ static int32_t create_impl(const ltri_paged_config* cfg, void* k_pages, void* v_
   b.err = (int32_t*)(c->state + L.err); b.tickets = (int32_t*)(c->state + L.tickets);
   b.lse2 = (float*)(t + L.lse); b.part = (float*)(t + L.part); b.part_ml = (unsigned long long*)(t + L.part_ml); b.scores = (float*)(t + L.scores);
   b.move_head = (long long*)(t + L.move_head); b.moves = (int32_t*)(t + L.moves);
+  b.keys = (uint32_t*)(t + L.keys); b.candidates = (uint32_t*)(t + L.candidates); b.long_slots = t + L.long_slots;
+  b.long_counts = (int32_t*)(t + L.long_counts); b.long_state = (int32_t*)(c->state + L.long_state);
   if (!dry) {
     hipError_t e = hipGetDevice(&c->device);
     if (e == hipSuccess) e = hipDeviceGetAttribute(&b.n_cus, hipDeviceAttributeMultiprocessorCount, c->device);

@@ -10,11 +10,17 @@ namespace ltri {
 constexpr int PAGED_TILE = 32;             // rows of scores are padded to at most this many tokens
 constexpr int PAGED_MAX_WGS = 1024;        // workgroups of an attention launch, at most
 
+// Eviction: tables of up to EV_LONG tokens are selected from by one workgroup per (sequence, KV head), longer ones by several.
+constexpr int EV_LONG = 32768, EV_CHUNK = 8192;
+constexpr int EV_LONG_WORDS = 4 + 2048;    // counters of a (sequence, KV head), zero between launches
+constexpr int EV_SLOT_BYTES = 24;          // what the launches of a long selection tell each other
+
 struct PagedDims {
   int Hq, Hkv, G, d, dtype, elt;
   int page_shift, n_pages, table_pages, max_seqs, rows_max, weights;
   long long page_stride, head_stride, token_stride;    // elements
   long long cap_tokens;                                // table_pages * page_tokens
+  int long_pieces;                                     // pieces of EV_CHUNK tokens of a table, and one
   long long score_tiles;                               // tiles of scores, and of lists of moves, the scratch has room for
 };
 
@@ -22,6 +28,7 @@ struct PagedDims {
 struct PagedLayout {
   size_t err;          // int32 [4]
   size_t tickets;      // int32 [max_seqs][Hkv][blocks of 16 pairs]  zero between launches
+  size_t long_state;   // int32 [max_seqs * Hkv][EV_LONG_WORDS]  zero between launches (tables of more than EV_LONG tokens)
   size_t state_total;
   size_t lse;          // float [max_seqs][rows_max][Hq]  log-sum-exp, log2 domain
   size_t part;         // float [2 PAGED_MAX_WGS][16][d]  partial results of a workgroup's first and last problem
@@ -29,6 +36,9 @@ struct PagedLayout {
   size_t scores;       // float [score_tiles][Hkv][rows_max * G][PAGED_TILE]   (ordered otherwise, see score_rows)
   size_t move_head;    // int64 [max_seqs * Hkv][2]  offset of a list of moves and its length
   size_t moves;        // int32 [score_tiles][Hkv][PAGED_TILE]
+  size_t keys, candidates;   // uint32, the same (tables of more than EV_LONG tokens, and the next two)
+  size_t long_slots;   // [max_seqs * Hkv] of EV_SLOT_BYTES
+  size_t long_counts;  // int32 [max_seqs * Hkv][long_pieces][2]
   size_t scratch_total;
 };
 
@@ -37,6 +47,7 @@ struct PagedCall {
   char* k; char* v; float* weight; int32_t* pos;
   int32_t* err; int32_t* tickets;
   float* lse2; float* part; unsigned long long* part_ml; float* scores; long long* move_head; int32_t* moves;
+  uint32_t* keys; uint32_t* candidates; char* long_slots; int32_t* long_counts; int32_t* long_state;
   const int32_t* table; int32_t* lens; const int32_t* seen;
   int seq_count;
   int n_cus;                 // compute units of the device

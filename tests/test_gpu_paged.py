@@ -272,10 +272,16 @@ def test_evict_rows_of_every_width(gpu_device, dtype, dim, token_major):
     check_evict(c, 75, 4, 20)
 
 
-@pytest.mark.parametrize("keep", [60000, 139000, 500])
-def test_evict_long(gpu_device, keep):
-    c = evict_case(gpu_device, [140000, 3000, 70001], "any", hq=2, hkv=2, dim=64, page=64)
+@pytest.mark.parametrize("kind,keep,lens", [
+    ("any", 60000, [140000, 3000, 70001]), ("any", 139000, [140000, 139001, 500]), ("any", 500, [90000, 501, 0]), ("ties", 40000, [90000, 40001]),
+    ("zero", 8192, [70000, 8193, 16384]), ("odd", 30000, [50000]), ("signed", 32768, [65536, 32769]), ("odd", 33000, [41000, 40900]),
+])
+def test_evict_long(gpu_device, kind, keep, lens):
+    """Tables that several workgroups select from."""
+    c = evict_case(gpu_device, lens, kind, hq=2, hkv=2, dim=64, page=64)
     check_evict(c, keep, 4, 300)
+    check_evict(c, keep, 4, 300)
+    check_evict(c, keep // 2, 0, 7)
 
 
 def test_positions_that_repeat_keep_the_count(gpu_device):
