@@ -86,15 +86,15 @@ static int32_t derive(const ltri_paged_config* cfg, PagedDims& D, PagedLayout& L
   D.score_tiles = 0;
   D.long_pieces = (int)((D.cap_tokens + EV_CHUNK - 1) / EV_CHUNK + 1);    // (one more: pieces end at the budget)
   if (D.weights) {
-    const long long pool = (((long long)c.n_pages << D.page_shift) + PAGED_TILE - 1) / PAGED_TILE + c.max_seqs;
-    const long long tables = (D.cap_tokens + PAGED_TILE - 1) / PAGED_TILE * c.max_seqs;
+    const long long pool = (((long long)c.n_pages << D.page_shift) + PAGED_TILE - 1) / PAGED_TILE + (long long)c.max_seqs * (1 + PAGED_EXTRA);
+    const long long tables = ((D.cap_tokens + PAGED_TILE - 1) / PAGED_TILE + PAGED_EXTRA) * c.max_seqs;
     D.score_tiles = pool < tables ? pool : tables;
   }
   if ((double)D.score_tiles * D.Hq * D.rows_max * PAGED_TILE * 4 > 1e15) return LTRI_EINVAL;
   o = 0;
   L.lse = o;    o = align_up(o + (size_t)c.max_seqs * D.rows_max * D.Hq * 4);
-  L.part = o;   o = align_up(o + (size_t)2 * PAGED_MAX_WGS * 16 * D.d * 4);
-  L.part_ml = o; o = align_up(o + (size_t)2 * PAGED_MAX_WGS * 16 * 8);
+  L.part = o;   o = align_up(o + (size_t)2 * PAGED_MAX_WGS * 32 * D.d * 4);
+  L.part_ml = o; o = align_up(o + (size_t)2 * PAGED_MAX_WGS * 32 * 8);
   L.scores = o; o = align_up(o + (size_t)D.score_tiles * D.Hq * D.rows_max * PAGED_TILE * 4);
   const size_t attend_end = o;
   o = 0;                                                 // the two kinds of call share the scratch

@@ -8,6 +8,7 @@
 namespace ltri {
 
 constexpr int PAGED_TILE = 32;             // rows of scores are padded to at most this many tokens
+constexpr int PAGED_EXTRA = 4;             // tiles that the beginning and end of a (sequence, KV head, block of pairs) are as long as
 constexpr int PAGED_MAX_WGS = 1024;        // workgroups of an attention launch, at most
 
 // Eviction: tables of up to EV_LONG tokens are selected from by one workgroup per (sequence, KV head), longer ones by several.
@@ -31,8 +32,8 @@ struct PagedLayout {
   size_t long_state;   // int32 [max_seqs * Hkv][EV_LONG_WORDS]  zero between launches (tables of more than EV_LONG tokens)
   size_t state_total;
   size_t lse;          // float [max_seqs][rows_max][Hq]  log-sum-exp, log2 domain
-  size_t part;         // float [2 PAGED_MAX_WGS][16][d]  partial results of a workgroup's first and last problem
-  size_t part_ml;      // float2 [2 PAGED_MAX_WGS][16]    their maxima and sums
+  size_t part;         // float [2 PAGED_MAX_WGS][32][d]  partial results of a workgroup's first and last problem
+  size_t part_ml;      // float2 [2 PAGED_MAX_WGS][32]    their maxima and sums
   size_t scores;       // float [score_tiles][Hkv][rows_max * G][PAGED_TILE]   (ordered otherwise, see score_rows)
   size_t move_head;    // int64 [max_seqs * Hkv][2]  offset of a list of moves and its length
   size_t moves;        // int32 [score_tiles][Hkv][PAGED_TILE]
