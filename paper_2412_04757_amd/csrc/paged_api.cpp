@@ -92,10 +92,12 @@ static int32_t derive(const ltri_paged_config* cfg, PagedDims& D, PagedLayout& L
   }
   if ((double)D.score_tiles * D.Hq * D.rows_max * PAGED_TILE * 4 > 1e15) return LTRI_EINVAL;
   o = 0;
+  const int pairs = D.rows_max * D.G, block = pairs <= 16 ? 16 : pairs <= 32 ? 32 : 64;      // of a problem, at most
+  const int scored = pairs < PAGED_SCORE_PAIRS ? pairs : PAGED_SCORE_PAIRS;                  // pairs whose scores are kept, at most
   L.lse = o;    o = align_up(o + (size_t)c.max_seqs * D.rows_max * D.Hq * 4);
-  L.part = o;   o = align_up(o + (size_t)2 * PAGED_MAX_WGS * 32 * D.d * 4);
-  L.part_ml = o; o = align_up(o + (size_t)2 * PAGED_MAX_WGS * 32 * 8);
-  L.scores = o; o = align_up(o + (size_t)D.score_tiles * D.Hq * D.rows_max * PAGED_TILE * 4);
+  L.part = o;   o = align_up(o + (size_t)2 * PAGED_MAX_WGS * block * D.d * 4);
+  L.part_ml = o; o = align_up(o + (size_t)2 * PAGED_MAX_WGS * block * 8);
+  L.scores = o; o = align_up(o + (size_t)D.score_tiles * D.Hkv * scored * PAGED_TILE * 4);
   const size_t attend_end = o;
   o = 0;                                                 // the two kinds of call share the scratch
   L.move_head = o; o = align_up(o + (D.weights ? (size_t)c.max_seqs * D.Hkv * 16 : 0));

@@ -25,8 +25,6 @@ namespace ltri {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int PA_WAVES = 4;
-// Workgroups of a compute unit, by registers (their tiles and results: 112 at head_dim 128 with one block of pairs, 160 with two).
-constexpr int paged_occupancy(int dim, int blocks) { return dim == 128 && blocks == 2 ? 1 : 2; }
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
@@ -37,6 +35,8 @@ __host__ __device__ __forceinline__ int pair_blocks(const PagedCall& a, int size
 __device__ __forceinline__ int tiles_of(int len, int tile) { return (len + tile - 1) / tile; }
 // What a problem counts as when work is shared out: its tiles and PAGED_EXTRA, which its beginning and end cost.
 __device__ __forceinline__ int units_of(int len, int tile) { return len ? tiles_of(len, tile) + PAGED_EXTRA : 0; }
+
+__device__ __forceinline__ long long share_of(long long total, int wgs, int min_share) { return max((total + wgs - 1) / wgs, (long long)min_share); }
 
 // Scores of sequence s: [KV head][pair][tokens, padded to the tile], behind the units of the sequences in front; NULL: no room.
 __device__ __forceinline__ float* score_rows(const PagedCall& a, long long before, int nt, int tile, int h) {
@@ -75,17 +75,17 @@ __device__ __forceinline__ float second_float(unsigned long long v) { return __u
 __device__ __forceinline__ float safe_ref(float m) { return m == -INFINITY ? 0.f : m; }
 
 // A wavefront's matrix products of one tile, by type. NU: groups of 16 tokens in a tile; VW: 32-bit words of a lane's piece of a value row.
-// NB: blocks of 16 pairs that share a tile's rows.
-template <int DT, int DIM, int NB> struct TileOps;
+template <int DT, int DIM> struct TileOps;
 
-template <int DIM, int NB> struct TileOps<LTRI_BF16, DIM, NB> {
+template <int DIM> struct TileOps<LTRI_BF16, DIM> {
   static constexpr int NU = 2, NK = DIM / 32, NT = DIM / 16, CP = NT, VW = CP / 2;
-  u32x4_t q[NB][NK], k[NU][NK];
+  typedef u32x4_t Piece;
+  Piece q[NK], k[NU][NK];
   uint32_t v[NU][4][VW];
-  f32x4_t o[NB][NT];
-  __device__ __forceinline__ void load_q(int b, const char* row, int g, bool there) {
+  f32x4_t o[NT];
+  __device__ __forceinline__ void load_q(const char* row, int g, bool there) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) q[b][i] = there ? *(const u32x4_t*)(row + i * 64 + g * 16) : u32x4_t{0u, 0u, 0u, 0u};
+    for (int i = 0; i < NK; ++i) q[i] = there ? *(const u32x4_t*)(row + i * 64 + g * 16) : u32x4_t{0u, 0u, 0u, 0u};
   }
   __device__ __forceinline__ void load_k(int u, const char* row, int g) {            // row: of token 16 u + lane % 16
 #pragma unroll
@@ -113,32 +113,28 @@ template <int DIM, int NB> struct TileOps<LTRI_BF16, DIM, NB> {
     for (int w = 0; w < VW; ++w) odd |= not_finite_bf16x2(v[u][j][w]);
     return odd;
   }
-  __device__ __forceinline__ void scores(f32x4_t (&s)[NB][NU]) const {
+  __device__ __forceinline__ void scores(f32x4_t (&s)[NU]) const {
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+    for (int u = 0; u < NU; ++u) {
+      s[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int u = 0; u < NU; ++u) {
-        s[b][u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < NK; ++i)
-          s[b][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[u][i]), __builtin_bit_cast(bf16x8_t, q[b][i]), s[b][u], 0, 0, 0);
-      }
+      for (int i = 0; i < NK; ++i)
+        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[u][i]), __builtin_bit_cast(bf16x8_t, q[i]), s[u], 0, 0, 0);
+    }
   }
-  // o += V^T P^T. APART: only the lane's tokens [u][j] whose bit 4 u + j of vis is set count, and only the pairs of lanes with mine[b] take the sum.
+  // o += V^T P^T. APART: only the lane's tokens [u][j] whose bit 4 u + j of vis is set count, and only the pairs of lanes with `mine` take the sum.
   template <bool APART>
-  __device__ __forceinline__ void values(const f32x4_t (&p)[NB][NU], uint32_t vis, const bool (&mine)[NB]) {
-    u32x4_t hi[NB], lo[NB];
+  __device__ __forceinline__ void values(const f32x4_t (&p)[NU], uint32_t vis, bool mine) {
+    u32x4_t hi, lo;
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
-      for (int u = 0; u < NU; ++u)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const float x = p[b][u][2 * c], y = p[b][u][2 * c + 1];
-          const uint32_t h = pack2(x, y);
-          hi[b][2 * u + c] = h;
-          lo[b][2 * u + c] = pack2(x - __uint_as_float(h << 16), y - __uint_as_float(h & 0xFFFF0000u));
-        }
+      for (int c = 0; c < 2; ++c) {
+        const float x = p[u][2 * c], y = p[u][2 * c + 1];
+        const uint32_t h = pack2(x, y);
+        hi[2 * u + c] = h;
+        lo[2 * u + c] = pack2(x - __uint_as_float(h << 16), y - __uint_as_float(h & 0xFFFF0000u));
+      }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       u32x4_t col;
@@ -151,29 +147,27 @@ template <int DIM, int NB> struct TileOps<LTRI_BF16, DIM, NB> {
           col[2 * u + c] = x;
         }
       const bf16x8_t A = __builtin_bit_cast(bf16x8_t, col);
+      f32x4_t sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, __builtin_bit_cast(bf16x8_t, lo), o[t], 0, 0, 0);
+      sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, __builtin_bit_cast(bf16x8_t, hi), sum, 0, 0, 0);
+      if constexpr (APART) {
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        f32x4_t sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, __builtin_bit_cast(bf16x8_t, lo[b]), o[b][t], 0, 0, 0);
-        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, __builtin_bit_cast(bf16x8_t, hi[b]), sum, 0, 0, 0);
-        if constexpr (APART) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[b][t][e] = mine[b] ? sum[e] : o[b][t][e];
-        } else {
-          o[b][t] = sum;
-        }
+        for (int e = 0; e < 4; ++e) o[t][e] = mine ? sum[e] : o[t][e];
+      } else {
+        o[t] = sum;
       }
     }
   }
 };
 
-template <int DIM, int NB> struct TileOps<LTRI_F32, DIM, NB> {
+template <int DIM> struct TileOps<LTRI_F32, DIM> {
   static constexpr int NU = 1, NK = DIM / 16, NT = DIM / 16, CP = 4, VW = DIM / 16;
-  f32x4_t q[NB][NK], k[NU][NK];
+  typedef f32x4_t Piece;
+  Piece q[NK], k[NU][NK];
   uint32_t v[NU][4][VW];
-  f32x4_t o[NB][NT];
-  __device__ __forceinline__ void load_q(int b, const char* row, int g, bool there) {
+  f32x4_t o[NT];
+  __device__ __forceinline__ void load_q(const char* row, int g, bool there) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) q[b][i] = there ? *(const f32x4_t*)(row + i * 64 + g * 16) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < NK; ++i) q[i] = there ? *(const f32x4_t*)(row + i * 64 + g * 16) : f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
   __device__ __forceinline__ void load_k(int u, const char* row, int g) {
 #pragma unroll
@@ -205,46 +199,93 @@ template <int DIM, int NB> struct TileOps<LTRI_F32, DIM, NB> {
     for (int w = 0; w < VW; ++w) odd |= not_finite_f32(v[u][j][w]);
     return odd;
   }
-  __device__ __forceinline__ void scores(f32x4_t (&s)[NB][NU]) const {
+  __device__ __forceinline__ void scores(f32x4_t (&s)[NU]) const {
+    s[0] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      s[b][0] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < NK; ++i)
 #pragma unroll
-      for (int i = 0; i < NK; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[b][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[0][i][e], q[b][i][e], s[b][0], 0, 0, 0);
-    }
+      for (int e = 0; e < 4; ++e) s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[0][i][e], q[i][e], s[0], 0, 0, 0);
   }
   template <bool APART>
-  __device__ __forceinline__ void values(const f32x4_t (&p)[NB][NU], uint32_t vis, const bool (&mine)[NB]) {
+  __device__ __forceinline__ void values(const f32x4_t (&p)[NU], uint32_t vis, bool mine) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+    for (int t = 0; t < NT; ++t) {
+      f32x4_t sum = o[t];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        f32x4_t sum = o[b][t];
+      for (int j = 0; j < 4; ++j)
+        sum = __builtin_amdgcn_mfma_f32_16x16x4f32(!APART || ((vis >> j) & 1) ? __uint_as_float(v[0][j][t]) : 0.f, p[0][j], sum, 0, 0, 0);
+      if constexpr (APART) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          sum = __builtin_amdgcn_mfma_f32_16x16x4f32(!APART || ((vis >> j) & 1) ? __uint_as_float(v[0][j][t]) : 0.f, p[b][0][j], sum, 0, 0, 0);
-        if constexpr (APART) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[b][t][e] = mine[b] ? sum[e] : o[b][t][e];
-        } else {
-          o[b][t] = sum;
-        }
+        for (int e = 0; e < 4; ++e) o[t][e] = mine ? sum[e] : o[t][e];
+      } else {
+        o[t] = sum;
       }
+    }
   }
 };
 
+// Sum of a problem's partial results of four columns of a pair: the parts first, first + step, ..., eight in flight. block: pairs of a problem.
+template <int DIM>
+__device__ __forceinline__ void add_parts(const PagedCall& a, int block, int w0, int parts, int first, int step, int p, int c, f32x4_t& o, float& top,
+                                          float& sum) {
+  constexpr int DEEP = 8;
+  top = -INFINITY;
+  sum = 0.f;
+  o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int k0 = first; k0 < parts; k0 += step * DEEP) {
+    unsigned long long ml[DEEP], lo[DEEP], hi[DEEP];
+#pragma unroll
+    for (int u = 0; u < DEEP; ++u) {
+      const int k = min(k0 + step * u, parts - 1);
+      const size_t at_part = (2 * (size_t)(w0 + k) + (k == 0)) * block + p;
+      const unsigned long long* from = (const unsigned long long*)(a.part + at_part * DIM + c);
+      ml[u] = __hip_atomic_load(a.part_ml + at_part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      lo[u] = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      hi[u] = __hip_atomic_load(from + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    float most = top;
+#pragma unroll
+    for (int u = 0; u < DEEP; ++u) most = fmaxf(most, first_float(ml[u]));     // (past the end: the last part's again)
+    const float ref = safe_ref(most), back = __builtin_amdgcn_exp2f(top - ref);
+    sum *= back;
+    o *= back;
+    top = most;
+#pragma unroll
+    for (int u = 0; u < DEEP; ++u) {
+      if (k0 + step * u >= parts) continue;
+      const float e = __builtin_amdgcn_exp2f(first_float(ml[u]) - ref);
+      sum = fmaf(e, second_float(ml[u]), sum);
+      o += e * f32x4_t{first_float(lo[u]), second_float(lo[u]), first_float(hi[u]), second_float(hi[u])};
+    }
+  }
+}
+
+// A result's four columns, and with the first of them its log-sum-exp.
+template <int DT, int DIM>
+__device__ __forceinline__ void write_result(const PagedCall& a, size_t r, int c, f32x4_t o, float top, float sum) {
+  if (sum == 0.f) o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  else o *= 1.f / sum;
+  if constexpr (DT == LTRI_F32) *(f32x4_t*)((float*)a.out + r * DIM + c) = o;
+  else *(uint2*)((uint16_t*)a.out + r * DIM + c) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
+  if (c == 0) {
+    const float lse2 = sum == 0.f ? -INFINITY : top + log2f(sum);
+    a.lse2[r] = lse2;
+    if (a.lse) a.lse[r] = lse2 * LN2;
+  }
+}
+
+// WB blocks of 16 pairs to a problem: a wavefront has block wave % WB, and every (PA_WAVES / WB)-th tile of the share. The blocks' wavefronts go through
+// the same tiles side by side, so that one reads from memory what the others find in the compute unit's cache.
 // SMALL: pages of fewer than 16 tokens, whose page is looked up lane by lane; else a group of 16 tokens lies in one page.
-template <int DT, int DIM, int NB, bool SMALL>
-__global__ __launch_bounds__(64 * PA_WAVES, paged_occupancy(DIM, NB)) void paged_attend_kernel(PagedCall a, int min_share) {
-  typedef TileOps<DT, DIM, NB> Ops;
+template <int DT, int DIM, int WB, bool SMALL>
+__global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCall a, int min_share, int merge_later) {
+  typedef TileOps<DT, DIM> Ops;
   constexpr int T = PagedTile<DT>::N, NU = Ops::NU, NT = Ops::NT, CP = Ops::CP, ELT = DT == LTRI_F32 ? 4 : 2;
   constexpr int PITCH = DIM + 4;
   static_assert(NU * 16 == T && WALK_T == 64 * PA_WAVES, "");
-  constexpr int PB = 16 * NB;                    // pairs of a problem
-  __shared__ __align__(16) float s_o[PA_WAVES][PB][PITCH];
-  __shared__ float s_m[PA_WAVES][PB], s_l[PA_WAVES][PB];
+  constexpr int PB = 16 * WB, STEP = PA_WAVES / WB;                  // pairs of a problem, wavefronts of a block
+  __shared__ __align__(16) float s_o[PA_WAVES][16][PITCH];
+  __shared__ float s_m[PA_WAVES][16], s_l[PA_WAVES][16];
   __shared__ int s_last;
   const PagedDims& D = a.D;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kl = lane & 15, g = lane >> 4;
@@ -258,7 +299,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, paged_occupancy(DIM, NB)) void paged
   long long share = 0;
   const PagedPlace at = paged_find(a.seq_count, [&](int s) { return (long long)units_of(paged_len(a, s), T) * per_tile; },
                                    [&](long long total) {
-                                     share = max((total + gridDim.x - 1) / gridDim.x, (long long)min_share);
+                                     share = share_of(total, gridDim.x, min_share);
                                      return share * w;
                                    });
   // sequences without tokens
@@ -290,31 +331,26 @@ __global__ __launch_bounds__(64 * PA_WAVES, paged_occupancy(DIM, NB)) void paged
 
     const int first_new = a.k_new ? max(len - a.n, 0) : len;         // tokens from here on come with the call
     const int np = min(PB, pairs - pb * PB);
-    const int all_see = len - a.n + 1 + pb * PB / D.G;               // tokens that every pair of the block sees
+    const int pair0 = pb * PB + 16 * (wave % WB);                    // the wavefront's pairs: from here on
+    const int pair = min(pair0 + kl, pairs - 1), query_row = pair / D.G;
+    const int sees = len - a.n + 1 + query_row;                      // tokens that the lane's pair sees
+    const int all_see = len - a.n + 1 + min(pair0, pairs - 1) / D.G; // ... that every pair of the block sees
     // tiles from here on: some token is not seen by some pair, or comes with the call (SMALL: every tile takes that way)
     const int first_edge = SMALL ? t0 : max(0, min(all_see, first_new)) / T;
     const int32_t* table = a.table + (size_t)s * D.table_pages;
     const char* kh = a.k + (size_t)h * D.head_stride * ELT;
     const char* vh = a.v + (size_t)h * D.head_stride * ELT;
     float* scores = nullptr;
-    if (a.decay >= 0.f) {
+    if (a.decay >= 0.f && paged_keeps_scores(pairs)) {
       scores = score_rows(a, before / per_tile, nt, T, h);
-      if (scores) scores += (size_t)(pb * PB + kl) * nt * T + 4 * g;
+      if (scores) scores += (size_t)(pair0 + kl) * nt * T + 4 * g;
     }
 
     Ops ops;
-    float m[NB], l[NB];
-    int row_of[NB];                                                  // query rows of the lane's pairs
+    ops.load_q((const char*)a.q + (((size_t)s * a.n + query_row) * D.Hq + h * D.G + pair % D.G) * DIM * ELT, g, pair0 + kl < pairs);
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int pair = min(pb * PB + 16 * b + kl, pairs - 1);
-      row_of[b] = pair / D.G;
-      ops.load_q(b, (const char*)a.q + (((size_t)s * a.n + row_of[b]) * D.Hq + h * D.G + pair % D.G) * DIM * ELT, g, 16 * b + kl < np);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) ops.o[b][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      m[b] = -INFINITY;
-      l[b] = 0.f;
-    }
+    for (int t = 0; t < NT; ++t) ops.o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
 
     // Pages of a tile: of its groups of 16 tokens, by scalar loads (the table does not change while a launch runs), or (SMALL) of the token that
     // the lane loads of every group's keys and of its four of the values. Past the sequence's end the last token's. They are asked for before the
@@ -372,37 +408,34 @@ __global__ __launch_bounds__(64 * PA_WAVES, paged_occupancy(DIM, NB)) void paged
     // One tile; EDGE: see first_edge.
     auto tile = [&](int t, auto edge_c) __attribute__((always_inline)) {
       constexpr bool EDGE = decltype(edge_c)::value;
-      f32x4_t sv[NB][NU];
+      f32x4_t sv[NU];
       const int kl_ = EDGE ? only_here(kl) : kl, g_ = EDGE ? only_here(g) : g;
+      const bool writes = EDGE && a.k_new && pb == 0 && wave % WB == 0;
       ops.scores(sv);
-      if constexpr (EDGE) {
-        if (pb == 0 && a.k_new) {
+      if (writes) {
 #pragma unroll
-          for (int u = 0; u < NU; ++u) {
-            const int i = t * T + 16 * u + kl_;
-            const int page = i >= first_new && i < len ? paged_page(a, s, i) : -1;
-            if (page < 0) continue;
-            ops.store_k(u, const_cast<char*>(row(kh, page, i)), g_);
-            if (D.weights && g_ == 0) {
-              const size_t mark = paged_mark(D, page, h, i);
-              a.weight[mark] = 0.f;
-              a.pos[mark] = a.seen[s] - (len - i);
-            }
+        for (int u = 0; u < NU; ++u) {
+          const int i = t * T + 16 * u + kl_;
+          const int page = i >= first_new && i < len ? paged_page(a, s, i) : -1;
+          if (page < 0) continue;
+          ops.store_k(u, const_cast<char*>(row(kh, page, i)), g_);
+          if (D.weights && g_ == 0) {
+            const size_t mark = paged_mark(D, page, h, i);
+            a.weight[mark] = 0.f;
+            a.pos[mark] = a.seen[s] - (len - i);
           }
         }
       }
-      const bool more = t + PA_WAVES < t1;
+      const bool more = t + STEP < t1;
       Pages after;
-      look_up(min(t + 2 * PA_WAVES, nt - 1), after);
-      if (more) load_k(t + PA_WAVES, next);
+      look_up(min(t + 2 * STEP, nt - 1), after);
+      if (more) load_k(t + STEP, next);
       __builtin_amdgcn_sched_barrier(0);
 
-      // of the lane's tokens 16 u + 4 g + j (bit 4 u + j): which are there at all, and which block b's pair sees
-      uint32_t there = 0xFFu, vis[NB];
+      // of the lane's tokens 16 u + 4 g + j (bit 4 u + j): which are there at all, and which its pair sees
+      uint32_t there = 0xFFu, vis = 0xFFu;
       if constexpr (EDGE) {
-        there = 0u;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) vis[b] = 0u;
+        there = vis = 0u;
 #pragma unroll
         for (int u = 0; u < NU; ++u)
 #pragma unroll
@@ -411,8 +444,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, paged_occupancy(DIM, NB)) void paged
             const bool ok = i < len && good(now.v[u][SMALL ? j : 0]);
             if (i < len && !ok) atomicCAS(a.err, 0, LTRI_EINVAL);
             there |= (uint32_t)ok << (4 * u + j);
-#pragma unroll
-            for (int b = 0; b < NB; ++b) vis[b] |= (uint32_t)(ok && i < len - a.n + 1 + row_of[b]) << (4 * u + j);
+            vis |= (uint32_t)(ok && i < sees) << (4 * u + j);
           }
       } else {
         bool bad = false;
@@ -423,49 +455,43 @@ __global__ __launch_bounds__(64 * PA_WAVES, paged_occupancy(DIM, NB)) void paged
 #pragma unroll
           for (int u = 0; u < NU; ++u)
             if (!good(now.k[u])) {
-              there &= ~(0xFu << (4 * u));
 #pragma unroll
               for (int j = 0; j < 4; ++j) ops.zero_v(u, j);
-#pragma unroll
-              for (int b = 0; b < NB; ++b) sv[b][u] = f32x4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+              sv[u] = f32x4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
             }
         }
       }
+      float mx = -INFINITY;
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        float mx = -INFINITY;
+      for (int u = 0; u < NU; ++u)
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            sv[b][u][j] *= sc;
-            if constexpr (EDGE) sv[b][u][j] = (vis[b] >> (4 * u + j)) & 1 ? sv[b][u][j] : -INFINITY;
-            mx = fmaxf(mx, sv[b][u][j]);
-          }
-        if (scores && 16 * b + kl < np) {
-#pragma unroll
-          for (int u = 0; u < NU; ++u) *(f32x4_t*)(scores + (size_t)(16 * b * nt + t) * T + 16 * u) = sv[b][u];
+        for (int j = 0; j < 4; ++j) {
+          sv[u][j] *= sc;
+          if constexpr (EDGE) sv[u][j] = (vis >> (4 * u + j)) & 1 ? sv[u][j] : -INFINITY;
+          mx = fmaxf(mx, sv[u][j]);
         }
-        const float m_new = fmaxf(m[b], max_quarters(mx)), ref = safe_ref(m_new);
-        if (__any(m_new > m[b])) {                                   // rare after the first tiles
-          const float alpha = __builtin_amdgcn_exp2f(m[b] - ref);
-          l[b] *= alpha;
+      if (scores && pair0 + kl < pairs) {
 #pragma unroll
-          for (int c = 0; c < NT; ++c) ops.o[b][c] *= alpha;
-          m[b] = m_new;
-        }
-#pragma unroll
-        for (int u = 0; u < NU; ++u)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            sv[b][u][j] = __builtin_amdgcn_exp2f(sv[b][u][j] - ref);
-            l[b] += sv[b][u][j];
-          }
+        for (int u = 0; u < NU; ++u) *(f32x4_t*)(scores + (size_t)t * T + 16 * u) = sv[u];
       }
-      bool mine[NB];
+      const float m_new = fmaxf(m, max_quarters(mx)), ref = safe_ref(m_new);
+      if (__any(m_new > m)) {                                        // rare after the first tiles
+        const float alpha = __builtin_amdgcn_exp2f(m - ref);
+        l *= alpha;
+#pragma unroll
+        for (int c = 0; c < NT; ++c) ops.o[c] *= alpha;
+        m = m_new;
+      }
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          sv[u][j] = __builtin_amdgcn_exp2f(sv[u][j] - ref);
+          l += sv[u][j];
+        }
       bool apart = false;                        // an infinity or NaN in a token that some pair of the block does not see
       if constexpr (EDGE) {
-        if (pb == 0 && a.k_new) {
+        if (writes) {
 #pragma unroll
           for (int u = 0; u < NU; ++u)
 #pragma unroll
@@ -485,89 +511,76 @@ __global__ __launch_bounds__(64 * PA_WAVES, paged_occupancy(DIM, NB)) void paged
         apart = (bool)__any(apart);
         if (apart) {
           // query row by query row, which takes the tokens it sees (0 times infinity would not be 0)
-          const int r0 = pb * PB / D.G, r1 = (pb * PB + np - 1) / D.G;
+          const int r0 = pair0 / D.G, r1 = min(pair0 + 15, pairs - 1) / D.G;
           for (int r = r0; r <= r1; ++r) {
             uint32_t seen_bits = 0u;
 #pragma unroll
             for (int u = 0; u < NU; ++u)
 #pragma unroll
               for (int j = 0; j < 4; ++j) seen_bits |= (uint32_t)(t * T + 16 * u + 4 * g_ + j < len - a.n + 1 + r) << (4 * u + j);
-#pragma unroll
-            for (int b = 0; b < NB; ++b) mine[b] = row_of[b] == r;
-            ops.template values<true>(sv, seen_bits, mine);
+            ops.template values<true>(sv, seen_bits, query_row == r);
           }
         }
       }
-      if (!apart) ops.template values<false>(sv, 0u, mine);
+      if (!apart) ops.template values<false>(sv, 0u, true);
       __builtin_amdgcn_sched_barrier(0);
-      if (more) load_v(t + PA_WAVES, next);
+      if (more) load_v(t + STEP, next);
       __builtin_amdgcn_sched_barrier(0);
       now = next;
       next = after;
     };
-    int t = t0 + wave;
+    int t = t0 + wave / WB;
+    if (pair0 >= pairs) t = t1;                                      // a block without pairs
     if (t < t1) {
       look_up(t, now);
-      look_up(min(t + PA_WAVES, nt - 1), next);
+      look_up(min(t + STEP, nt - 1), next);
       load_k(t, now);
       __builtin_amdgcn_sched_barrier(0);                             // keys before values, as in the loop: what is waited for first comes first
       load_v(t, now);
       __builtin_amdgcn_sched_barrier(0);
     }
-    for (; t < min(t1, first_edge); t += PA_WAVES) tile(t, std::false_type{});
-    for (; t < t1; t += PA_WAVES) tile(t, std::true_type{});
+    for (; t < min(t1, first_edge); t += STEP) tile(t, std::false_type{});
+    for (; t < t1; t += STEP) tile(t, std::true_type{});
 
-    // the four wavefronts' results: own maximum, sum and O
+    // the wavefronts' results: own maximum, sum and O
+    l = over_quarters(l);
     __syncthreads();                             // (the problem before has been read)
     const int tid_ = only_here(tid), lane_ = tid_ & 63, kl_ = lane_ & 15, g_ = lane_ >> 4;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int p = 16 * b + kl_;
-      l[b] = over_quarters(l[b]);
-      if (p >= np) continue;
+    if (pair0 + kl_ < pairs) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int c = 0; c < NT; c += 4) {
           const int col = 16 * CP * (c / CP) + CP * (4 * g_ + j) + c % CP;
-          *(f32x4_t*)&s_o[wave][p][col] = f32x4_t{ops.o[b][c][j], ops.o[b][c + 1][j], ops.o[b][c + 2][j], ops.o[b][c + 3][j]};
+          *(f32x4_t*)&s_o[wave][kl_][col] = f32x4_t{ops.o[c][j], ops.o[c + 1][j], ops.o[c + 2][j], ops.o[c + 3][j]};
         }
-      if (g_ == 0) { s_m[wave][p] = m[b]; s_l[wave][p] = l[b]; }
+      if (g_ == 0) { s_m[wave][kl_] = m; s_l[wave][kl_] = l; }
     }
     __syncthreads();
     const bool whole = t0 == 0 && t1 == nt;
     const size_t slot = 2 * (size_t)w + (t0 == 0);
-    // adds the four up, by threads that each take four columns of a pair, and hands (pair, column, O, maximum, sum) on
+    // adds up those of a block, by threads that each take four columns of a pair, and hands (pair, column, O, maximum, sum) on
     auto join = [&](auto take) __attribute__((always_inline)) {
       for (int i = tid_; i < np * (DIM / 4); i += WALK_T) {
-        const int p = i / (DIM / 4), c = i % (DIM / 4) * 4;
-        float top = s_m[0][p];
+        const int p = i / (DIM / 4), c = i % (DIM / 4) * 4, w0 = p / 16, pl = p % 16;
+        float top = s_m[w0][pl];
 #pragma unroll
-        for (int k = 1; k < PA_WAVES; ++k) top = fmaxf(top, s_m[k][p]);
+        for (int k = 1; k < STEP; ++k) top = fmaxf(top, s_m[w0 + k * WB][pl]);
         const float ref = safe_ref(top);
         float sum = 0.f;
         f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < PA_WAVES; ++k) {
-          const float e = __builtin_amdgcn_exp2f(s_m[k][p] - ref);
-          sum = fmaf(e, s_l[k][p], sum);
-          o += e * *(const f32x4_t*)&s_o[k][p][c];
+        for (int k = 0; k < STEP; ++k) {
+          const float e = __builtin_amdgcn_exp2f(s_m[w0 + k * WB][pl] - ref);
+          sum = fmaf(e, s_l[w0 + k * WB][pl], sum);
+          o += e * *(const f32x4_t*)&s_o[w0 + k * WB][pl][c];
         }
         take(p, c, o, top, sum);
       }
     };
     auto result = [&](int p, int c, f32x4_t o, float top, float sum) __attribute__((always_inline)) {
       const int pr = pb * PB + p;
-      const size_t r = ((size_t)s * a.n + pr / D.G) * D.Hq + h * D.G + pr % D.G;
-      if (sum == 0.f) o = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      else o *= 1.f / sum;
-      if constexpr (DT == LTRI_F32) *(f32x4_t*)((float*)a.out + r * DIM + c) = o;
-      else *(uint2*)((uint16_t*)a.out + r * DIM + c) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
-      if (c == 0) {
-        const float lse2 = sum == 0.f ? -INFINITY : top + log2f(sum);
-        a.lse2[r] = lse2;
-        if (a.lse) a.lse[r] = lse2 * LN2;
-      }
+      write_result<DT, DIM>(a, ((size_t)s * a.n + pr / D.G) * D.Hq + h * D.G + pr % D.G, c, o, top, sum);
     };
     if (whole) {
       join(result);
@@ -580,6 +593,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, paged_occupancy(DIM, NB)) void paged
       if (c == 0) __hip_atomic_store(a.part_ml + slot * PB + p, two_floats(top, sum), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     });
     const int w0 = (int)(problem / share), parts = (int)((problem + nt - 1) / share) - w0 + 1;      // the workgroups that share the problem
+    if (merge_later) continue;
     wait_for_own_stores();
     __syncthreads();
     int32_t* ticket = a.tickets + ((size_t)s * D.Hkv + h) * blocks + pb;
@@ -587,65 +601,92 @@ __global__ __launch_bounds__(64 * PA_WAVES, paged_occupancy(DIM, NB)) void paged
     __syncthreads();
     if (!s_last) continue;
     if (tid == 0) *ticket = 0;
-    // the parts, every fourth by one wavefront, DEEP in flight; then the four wavefronts' sums as above
-    constexpr int DEEP = 8;
-    for (int i = lane_; i < np * (DIM / 4); i += 64) {
-      const int p = i / (DIM / 4), c = i % (DIM / 4) * 4;
-      float top = -INFINITY, sum = 0.f;
-      f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-      for (int k0 = wave; k0 < parts; k0 += PA_WAVES * DEEP) {
-        unsigned long long ml[DEEP], lo[DEEP], hi[DEEP];
-#pragma unroll
-        for (int u = 0; u < DEEP; ++u) {
-          const int k = min(k0 + PA_WAVES * u, parts - 1);
-          const size_t at_part = (2 * (size_t)(w0 + k) + (k == 0)) * PB + p;
-          const unsigned long long* from = (const unsigned long long*)(a.part + at_part * DIM + c);
-          ml[u] = __hip_atomic_load(a.part_ml + at_part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          lo[u] = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          hi[u] = __hip_atomic_load(from + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        float most = top;
-#pragma unroll
-        for (int u = 0; u < DEEP; ++u) most = fmaxf(most, first_float(ml[u]));     // (past the end: the last part's again)
-        const float ref = safe_ref(most), back = __builtin_amdgcn_exp2f(top - ref);
-        sum *= back;
-        o *= back;
-        top = most;
-#pragma unroll
-        for (int u = 0; u < DEEP; ++u) {
-          if (k0 + PA_WAVES * u >= parts) continue;
-          const float e = __builtin_amdgcn_exp2f(first_float(ml[u]) - ref);
-          sum = fmaf(e, second_float(ml[u]), sum);
-          o += e * f32x4_t{first_float(lo[u]), second_float(lo[u]), first_float(hi[u]), second_float(hi[u])};
-        }
+    if constexpr (WB == 1) {                     // few pairs: every fourth part by one wavefront, then their sums as above
+      for (int i = lane_; i < np * (DIM / 4); i += 64) {
+        const int p = i / (DIM / 4), c = i % (DIM / 4) * 4;
+        f32x4_t o;
+        float top, sum;
+        add_parts<DIM>(a, PB, w0, parts, wave, PA_WAVES, p, c, o, top, sum);
+        *(f32x4_t*)&s_o[wave][p][c] = o;
+        if (c == 0) { s_m[wave][p] = top; s_l[wave][p] = sum; }
       }
-      *(f32x4_t*)&s_o[wave][p][c] = o;
-      if (c == 0) { s_m[wave][p] = top; s_l[wave][p] = sum; }
+      __syncthreads();
+      join(result);
+    } else {
+      for (int i = tid_; i < np * (DIM / 4); i += WALK_T) {
+        const int p = i / (DIM / 4), c = i % (DIM / 4) * 4;
+        f32x4_t o;
+        float top, sum;
+        add_parts<DIM>(a, PB, w0, parts, 0, 1, p, c, o, top, sum);
+        result(p, c, o, top, sum);
+      }
     }
-    __syncthreads();
-    join(result);
   }
 }
 
-// Weights from the scores: w <- decay w + sum over the KV head's pairs of exp(s - lse). A thread takes four tokens of a KV head;
-// pieces of 1024 tokens are shared out like the tiles above.
-constexpr int PW_TOKENS = 4 * WALK_T;
+// The partial results of problems that several workgroups share, a workgroup per query row and head: where there are many of them,
+// the workgroup that finishes last is too slow at it (128 KB through one compute unit take 9 us).
+template <int DT, int DIM>
+__global__ __launch_bounds__(WALK_T) void paged_merge_kernel(PagedCall a, int wgs, int min_share, int block) {
+  constexpr int T = PagedTile<DT>::N;
+  const PagedDims& D = a.D;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const size_t r = blockIdx.x;
+  const int head = (int)(r % D.Hq), q_row = (int)(r / D.Hq) % a.n, s = (int)(r / D.Hq / a.n), h = head / D.G, pair = q_row * D.G + head % D.G;
+  const int blocks = pair_blocks(a, block), per_tile = D.Hkv * blocks;
+  const int len = paged_len(a, s), nt = tiles_of(len, T);
+  if (len == 0) return;
+  const PagedPlace at = paged_place(a.seq_count, [&](int i) { return (long long)units_of(paged_len(a, i), T) * per_tile; }, s);
+  const long long share = share_of(at.total, wgs, min_share);
+  const long long problem = at.before + (long long)(h * blocks + pair / block) * (nt + PAGED_EXTRA) + PAGED_EXTRA;
+  const int w0 = (int)(problem / share), parts = (int)((problem + nt - 1) / share) - w0 + 1;
+  if (parts == 1) return;
+  __shared__ __align__(16) float s_o[WALK_T / 64][2][DIM];
+  __shared__ float s_m[WALK_T / 64][2], s_l[WALK_T / 64][2];
+  constexpr int LANES = DIM / 4, SIDES = 64 / LANES < 2 ? 1 : 2;               // the lanes of a wavefront that take other parts of the same columns
+  const int side = lane / LANES, c = lane % LANES * 4;
+  if (side < SIDES) {
+    f32x4_t o;
+    float top, sum;
+    add_parts<DIM>(a, block, w0, parts, wave * SIDES + side, WALK_T / 64 * SIDES, pair % block, c, o, top, sum);
+    *(f32x4_t*)&s_o[wave][side][c] = o;
+    if (c == 0) { s_m[wave][side] = top; s_l[wave][side] = sum; }
+  }
+  __syncthreads();
+  if (tid >= LANES) return;
+  float top = -INFINITY, sum = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < WALK_T / 64 * SIDES; ++k) top = fmaxf(top, s_m[k / SIDES][k % SIDES]);
+  const float ref = safe_ref(top);
+#pragma unroll
+  for (int k = 0; k < WALK_T / 64 * SIDES; ++k) {
+    const float e = __builtin_amdgcn_exp2f(s_m[k / SIDES][k % SIDES] - ref);
+    sum = fmaf(e, s_l[k / SIDES][k % SIDES], sum);
+    o += e * *(const f32x4_t*)&s_o[k / SIDES][k % SIDES][c];
+  }
+  write_result<DT, DIM>(a, r, c, o, top, sum);
+}
+
+// Weights from the scores: w <- decay w + sum over the KV head's pairs of exp(s - lse). A wavefront takes 256 tokens of a KV head at a
+// time, a lane four of them; the pieces are shared out like the tiles above.
+constexpr int PW_TOKENS = 256;
 template <int TILE>
 __global__ __launch_bounds__(WALK_T) void paged_weights_kernel(PagedCall a) {
   const PagedDims& D = a.D;
-  const int pairs = a.n * D.G, w = blockIdx.x;
+  const int pairs = a.n * D.G, w = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   auto pieces = [&](int len) { return (len + PW_TOKENS - 1) / PW_TOKENS; };
   long long share = 0;
   const PagedPlace at = paged_find(a.seq_count, [&](int s) { return (long long)pieces(paged_len(a, s)) * D.Hkv; },
                                    [&](long long total) { share = (total + gridDim.x - 1) / gridDim.x; return share * w; });
   if (at.seq < 0) return;
-  __shared__ float s_lse[LTRI_PAGED_MAX_ROWS * 128];
-  long long x = share * w, x_end = min(x + share, at.total), before = at.before;
   // units in front of the sequence
   long long units = paged_find(a.seq_count, [&](int s) { return s < at.seq ? (long long)units_of(paged_len(a, s), TILE) : 0; },
                                [&](long long) { return -1ll; }).total;
+  long long before = at.before;
+  const long long x_end = min(share * (w + 1), at.total);
   int s = at.seq;
-  while (x < x_end) {
+  for (long long x = share * w + wave; x < x_end;) {
     const int len = paged_len(a, s), nt = tiles_of(len, TILE), np = pieces(len);
     if (x >= before + (long long)np * D.Hkv) {
       before += (long long)np * D.Hkv;
@@ -654,26 +695,35 @@ __global__ __launch_bounds__(WALK_T) void paged_weights_kernel(PagedCall a) {
       continue;
     }
     const int h = (int)((x - before) / np), piece = (int)((x - before) % np);
-    ++x;
+    x += WALK_T / 64;
     const float* scores = score_rows(a, units, nt, TILE, h);
     if (!scores) {
-      if (threadIdx.x == 0) atomicCAS(a.err, 0, LTRI_ECAPACITY);
+      if (lane == 0) atomicCAS(a.err, 0, LTRI_ECAPACITY);
       continue;
     }
-    __syncthreads();
-    for (int p = threadIdx.x; p < pairs; p += WALK_T) s_lse[p] = a.lse2[((size_t)s * a.n + p / D.G) * D.Hq + h * D.G + p % D.G];
-    __syncthreads();
-    const int i0 = piece * PW_TOKENS + 4 * threadIdx.x;
+    const int i0 = piece * PW_TOKENS + 4 * lane, at_most = nt * TILE - 4;
+    const size_t pitch = (size_t)nt * TILE;
+    scores += min(i0, at_most);
+    const float* lse = a.lse2 + (size_t)s * a.n * D.Hq + h * D.G;
     f32x4_t got = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < pairs && i0 < len; ++p) {
-      const float lse2 = s_lse[p];
-      const f32x4_t v = *(const f32x4_t*)(scores + (size_t)p * nt * TILE + i0);
-      if (lse2 != -INFINITY) {
+    for (int p0 = 0; p0 < pairs; p0 += 4) {
+      f32x4_t v[4];
+      float l[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) got[j] += __builtin_amdgcn_exp2f(v[j] - lse2);
+      for (int u = 0; u < 4; ++u) {
+        const int p = min(p0 + u, pairs - 1);
+        l[u] = lse[(size_t)(p / D.G) * D.Hq + p % D.G];
+        v[u] = *(const f32x4_t*)(scores + p * pitch);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (p0 + u >= pairs || l[u] == -INFINITY) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) got[j] += __builtin_amdgcn_exp2f(v[u][j] - l[u]);
       }
     }
-    for (int j = 0; j < min(4, len - i0); ++j) {
+    for (int j = 0; j < 4; ++j) {
+      if (i0 + j >= len) break;
       const int page = paged_page(a, s, i0 + j);
       if (page < 0) continue;
       float* to = a.weight + paged_mark(D, page, h, i0 + j);
@@ -682,30 +732,164 @@ __global__ __launch_bounds__(WALK_T) void paged_weights_kernel(PagedCall a) {
   }
 }
 
-template <int DT, int DIM, int NB>
-static void launch_pages(const PagedCall& a, int wgs, int min_share, hipStream_t s) {
-  if (a.D.page_shift < 4) paged_attend_kernel<DT, DIM, NB, true><<<wgs, 64 * PA_WAVES, 0, s>>>(a, min_share);
-  else paged_attend_kernel<DT, DIM, NB, false><<<wgs, 64 * PA_WAVES, 0, s>>>(a, min_share);
-}
-template <int DT>
-static void launch_tiles(const PagedCall& a, bool two, int wgs, int min_share, hipStream_t s) {
-  if (a.D.d == 64) two ? launch_pages<DT, 64, 2>(a, wgs, min_share, s) : launch_pages<DT, 64, 1>(a, wgs, min_share, s);
-  else two ? launch_pages<DT, 128, 2>(a, wgs, min_share, s) : launch_pages<DT, 128, 1>(a, wgs, min_share, s);
+// The same from the keys, for many pairs (see paged_keeps_scores): the scores again, one tile of keys after the other, with the log-sum-exps at hand.
+// The queries of 64 pairs stay in registers; the next tile's keys are on their way while one is used.
+template <int DT, int DIM>
+__global__ __launch_bounds__(WALK_T, 2) void paged_key_weights_kernel(PagedCall a) {
+  constexpr int T = PagedTile<DT>::N, ELT = DT == LTRI_F32 ? 4 : 2, WAVES = WALK_T / 64, NB = 4;
+  typedef TileOps<DT, DIM> Ops;
+  constexpr int NU = Ops::NU;
+  const PagedDims& D = a.D;
+  const int pairs = a.n * D.G, w = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kl = lane & 15, g = lane >> 4;
+  const float sc = LOG2E / sqrtf((float)DIM);
+  const int tok_bytes = (int)D.token_stride * ELT;
+  long long share = 0;
+  const PagedPlace at = paged_find(a.seq_count, [&](int s) { return (long long)tiles_of(paged_len(a, s), T) * D.Hkv; },
+                                   [&](long long total) { share = share_of(total, gridDim.x, WAVES); return share * w; });
+  if (at.seq < 0) return;
+  long long x = share * w, before = at.before;
+  const long long x_end = min(x + share, at.total);
+  int s = at.seq;
+  while (x < x_end) {
+    const int len = paged_len(a, s), nt = tiles_of(len, T);
+    if (x >= before + (long long)nt * D.Hkv) {
+      before += (long long)nt * D.Hkv;
+      ++s;
+      continue;
+    }
+    const int h = (int)((x - before) / nt), t0 = (int)((x - before) % nt), t1 = (int)min((long long)nt, t0 + (x_end - x));
+    x += t1 - t0;
+    const int32_t* table = a.table + (size_t)s * D.table_pages;
+    const char* kh = a.k + h * D.head_stride * ELT;
+    struct Pages { int p[NU]; };                   // of the tokens 16 u + lane % 16; -1: none in the pool
+    auto look_up = [&](int t, Pages& p) {
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        p.p[u] = table[min(t * T + 16 * u + kl, len - 1) >> D.page_shift];
+        if ((unsigned)p.p[u] >= (unsigned)D.n_pages) p.p[u] = -1;
+      }
+    };
+    Ops ops;
+    auto load_k = [&](int t, const Pages& p) {
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        const int i = min(t * T + 16 * u + kl, len - 1);
+        ops.load_k(u, kh + (max(p.p[u], 0) * D.page_stride * ELT + (long long)(i & ((1 << D.page_shift) - 1)) * tok_bytes), g);
+      }
+    };
+    for (int p0 = 0; p0 < pairs; p0 += 16 * NB) {
+      typename Ops::Piece q[NB][Ops::NK];
+      float lse2[NB];
+      int sees[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int pair = min(p0 + 16 * b + kl, pairs - 1), row = pair / D.G;
+        const size_t r = ((size_t)s * a.n + row) * D.Hq + h * D.G + pair % D.G;
+        ops.load_q((const char*)a.q + r * DIM * ELT, g, true);
+#pragma unroll
+        for (int i = 0; i < Ops::NK; ++i) q[b][i] = ops.q[i];
+        lse2[b] = a.lse2[r];
+        sees[b] = p0 + 16 * b + kl < pairs && lse2[b] != -INFINITY ? len - a.n + 1 + row : 0;
+      }
+      int t = t0 + wave;
+      Pages now, next;
+      if (t < t1) {
+        look_up(t, now);
+        look_up(min(t + WAVES, nt - 1), next);
+        load_k(t, now);
+      }
+      for (; t < t1; t += WAVES) {
+        f32x4_t sv[NB][NU];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+          for (int i = 0; i < Ops::NK; ++i) ops.q[i] = q[b][i];
+          ops.scores(sv[b]);
+        }
+        Pages after;
+        look_up(min(t + 2 * WAVES, nt - 1), after);
+        if (t + WAVES < t1) load_k(t + WAVES, next);
+        // a lane's sums of its tokens 16 u + 4 g + j over the blocks, then over the 16 lanes that hold a token's pairs; lane 4 u + j keeps token 4 g + j of group u
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float got = 0.f;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) got += t * T + 16 * u + 4 * g + j < sees[b] ? __builtin_amdgcn_exp2f(fmaf(sv[b][u][j], sc, -lse2[b])) : 0.f;
+            got += __uint_as_float(lane_xor_c<8>(__float_as_uint(got)));
+            got += __uint_as_float(lane_xor_c<4>(__float_as_uint(got)));
+            got += __uint_as_float(lane_xor_c<2>(__float_as_uint(got)));
+            got += __uint_as_float(lane_xor_c<1>(__float_as_uint(got)));
+            if (kl == 4 * u + j) sum = got;
+          }
+        const int u = kl >> 2, i = t * T + 16 * u + 4 * g + (kl & 3);
+        const int page0 = __shfl(now.p[0], 4 * g + (kl & 3), 64), page1 = __shfl(now.p[NU - 1], 4 * g + (kl & 3), 64);
+        const int page = u == 0 ? page0 : page1;
+        if (u < NU && i < len && page >= 0) {
+          float* to = a.weight + paged_mark(D, page, h, i);
+          *to = p0 == 0 && a.decay == 0.f ? sum : fmaf(p0 == 0 ? a.decay : 1.f, *to, sum);
+        }
+        now = next;
+        next = after;
+      }
+    }
+  }
 }
 
+template <int DT, int DIM, int WB>
+static void launch_pages(const PagedCall& a, int wgs, int min_share, bool later, hipStream_t s) {
+  if (a.D.page_shift < 4) paged_attend_kernel<DT, DIM, WB, true><<<wgs, 64 * PA_WAVES, 0, s>>>(a, min_share, later);
+  else paged_attend_kernel<DT, DIM, WB, false><<<wgs, 64 * PA_WAVES, 0, s>>>(a, min_share, later);
+}
+template <int DT, int DIM>
+static void launch_blocks(const PagedCall& a, int wb, int wgs, int min_share, bool later, hipStream_t s) {
+  if (wb == 1) launch_pages<DT, DIM, 1>(a, wgs, min_share, later, s);
+  else if (wb == 2) launch_pages<DT, DIM, 2>(a, wgs, min_share, later, s);
+  else launch_pages<DT, DIM, 4>(a, wgs, min_share, later, s);
+}
+template <int DT>
+static void launch_dim(const PagedCall& a, int wb, int wgs, int min_share, bool later, hipStream_t s) {
+  if (a.D.d == 64) launch_blocks<DT, 64>(a, wb, wgs, min_share, later, s);
+  else launch_blocks<DT, 128>(a, wb, wgs, min_share, later, s);
+  if (!later) return;
+  const unsigned rows = (unsigned)a.seq_count * a.n * a.D.Hq;
+  if (a.D.d == 64) paged_merge_kernel<DT, 64><<<rows, WALK_T, 0, s>>>(a, wgs, min_share, 16 * wb);
+  else paged_merge_kernel<DT, 128><<<rows, WALK_T, 0, s>>>(a, wgs, min_share, 16 * wb);
+}
+template <int DT>
+static void launch_key_weights(const PagedCall& a, int wgs, hipStream_t s) {
+  if (a.D.d == 64) paged_key_weights_kernel<DT, 64><<<wgs, WALK_T, 0, s>>>(a);
+  else paged_key_weights_kernel<DT, 128><<<wgs, WALK_T, 0, s>>>(a);
+}
+
+// A launch of its own for the merge from this many bytes of a problem's partial results on. One sequence, 8 KV heads of 4: 128K tokens (131 KB) 107.5 us
+// with the last workgroup, 104.9 with the launch; 32K tokens of 16 rows (2 MB) 147 and 60; fp32, 2 x 4097 tokens of one KV head, 64 wide (66 KB) 12.7 and 15.3.
+constexpr long long MERGE_BYTES = 96 << 10;
+
 hipError_t launch_paged_attend(const PagedCall& a, hipStream_t s) {
-  const int tile = a.D.dtype == LTRI_F32 ? 16 : 32, min_share = PA_WAVES;
-  const bool two = a.n * a.D.G > 16;             // two blocks of pairs share the rows of a tile
+  const int tile = a.D.dtype == LTRI_F32 ? 16 : 32, pairs = a.n * a.D.G;
+  const int wb = pairs <= 16 ? 1 : pairs <= 32 ? 2 : 4, min_share = PA_WAVES / wb;
   // as many workgroups as the chip holds, or as the tables can have work for
-  const long long most = (long long)a.seq_count * a.D.Hkv * pair_blocks(a, two ? 32 : 16) * ((a.D.cap_tokens + tile - 1) / tile + PAGED_EXTRA);
-  const int wgs = (int)std::min<long long>(std::min(a.n_cus * paged_occupancy(a.D.d, two ? 2 : 1), PAGED_MAX_WGS), (most + min_share - 1) / min_share);
-  if (a.D.dtype == LTRI_F32) launch_tiles<LTRI_F32>(a, two, wgs, min_share, s);
-  else launch_tiles<LTRI_BF16>(a, two, wgs, min_share, s);
-  if (a.decay >= 0.f) {
+  const long long tiles = (long long)a.seq_count * a.D.Hkv * ((a.D.cap_tokens + tile - 1) / tile + PAGED_EXTRA);
+  const long long most = tiles * pair_blocks(a, 16 * wb);
+  const int wgs = (int)std::min<long long>(std::min(a.n_cus * 2, PAGED_MAX_WGS), (most + min_share - 1) / min_share);
+  // bytes of partial results of a problem, if its sequence is as long as the others
+  const long long problems = (long long)a.seq_count * a.D.Hkv * pair_blocks(a, 16 * wb);
+  const bool later = (wgs + problems - 1) / problems * std::min(pairs, 16 * wb) * a.D.d * 4 > MERGE_BYTES;
+  if (a.D.dtype == LTRI_F32) launch_dim<LTRI_F32>(a, wb, wgs, min_share, later, s);
+  else launch_dim<LTRI_BF16>(a, wb, wgs, min_share, later, s);
+  if (a.decay < 0.f) return hipGetLastError();
+  if (paged_keeps_scores(pairs)) {
     const long long pieces = (long long)a.seq_count * a.D.Hkv * ((a.D.cap_tokens + PW_TOKENS - 1) / PW_TOKENS);
-    const int n = (int)std::min<long long>(a.n_cus * 4, pieces);
+    const int n = (int)std::min<long long>(a.n_cus * 8, pieces);
     if (tile == 16) paged_weights_kernel<16><<<n, WALK_T, 0, s>>>(a);
     else paged_weights_kernel<32><<<n, WALK_T, 0, s>>>(a);
+  } else {
+    const int n = (int)std::min<long long>(a.n_cus * 2, (tiles + PA_WAVES - 1) / PA_WAVES);
+    if (a.D.dtype == LTRI_F32) launch_key_weights<LTRI_F32>(a, n, s);
+    else launch_key_weights<LTRI_BF16>(a, n, s);
   }
   return hipGetLastError();
 }

@@ -10,6 +10,11 @@ namespace ltri {
 constexpr int PAGED_TILE = 32;             // rows of scores are padded to at most this many tokens
 constexpr int PAGED_EXTRA = 4;             // tiles that the beginning and end of a (sequence, KV head, block of pairs) are as long as
 constexpr int PAGED_MAX_WGS = 1024;        // workgroups of an attention launch, at most
+// Whether an attention with weights leaves its scores in scratch for them (8 bytes a token and pair, written and read), or the keys are read
+// again (2 to 4 head_dim bytes a token): from 32 pairs on that is less, and the scratch need not hold scores of many rows.
+// 16 rows of 4 heads over 32K tokens, 8 KV heads: scores 54 us (20 of it their writes), keys 24; 4 rows: scores 16; 8 rows (32 pairs): keys 20.
+constexpr int PAGED_SCORE_PAIRS = 31;
+__host__ __device__ constexpr bool paged_keeps_scores(int pairs) { return pairs <= PAGED_SCORE_PAIRS; }
 
 // Eviction: tables of up to EV_LONG tokens are selected from by one workgroup per (sequence, KV head), longer ones by several.
 constexpr int EV_LONG = 32768, EV_CHUNK = 8192;
@@ -32,9 +37,9 @@ struct PagedLayout {
   size_t long_state;   // int32 [max_seqs * Hkv][EV_LONG_WORDS]  zero between launches (tables of more than EV_LONG tokens)
   size_t state_total;
   size_t lse;          // float [max_seqs][rows_max][Hq]  log-sum-exp, log2 domain
-  size_t part;         // float [2 PAGED_MAX_WGS][32][d]  partial results of a workgroup's first and last problem
-  size_t part_ml;      // float2 [2 PAGED_MAX_WGS][32]    their maxima and sums
-  size_t scores;       // float [score_tiles][Hkv][rows_max * G][PAGED_TILE]   (ordered otherwise, see score_rows)
+  size_t part;         // float [2 PAGED_MAX_WGS][16, 32 or 64][d]  partial results of a workgroup's first and last problem
+  size_t part_ml;      // float2 [2 PAGED_MAX_WGS][16, 32 or 64]    their maxima and sums
+  size_t scores;       // float [score_tiles][Hkv][pairs][PAGED_TILE]   (ordered otherwise, see score_rows)
   size_t move_head;    // int64 [max_seqs * Hkv][2]  offset of a list of moves and its length
   size_t moves;        // int32 [score_tiles][Hkv][PAGED_TILE]
   size_t keys, candidates;   // uint32, the same (tables of more than EV_LONG tokens, and the next two)

@@ -20,6 +20,7 @@ LENS = ([1], [0], [31, 32, 33], [0, 1, 700, 64, 0, 17], [5000], [2049, 3, 128, 1
 @pytest.mark.parametrize("dtype,dim,hq,hkv,page,rows", [
     ("bf16", 128, 8, 2, 16, 1), ("bf16", 128, 4, 4, 64, 1), ("bf16", 64, 8, 1, 1, 2), ("bf16", 128, 14, 2, 8, 3), ("bf16", 128, 32, 1, 32, 1),
     ("bf16", 64, 6, 2, 256, 16), ("f32", 64, 4, 1, 32, 1), ("f32", 128, 8, 2, 16, 4), ("f32", 128, 3, 3, 128, 1), ("bf16", 128, 8, 2, 2, 5),
+    ("f32", 128, 12, 2, 16, 7), ("f32", 64, 10, 2, 4, 6), ("bf16", 128, 10, 2, 64, 6), ("bf16", 64, 31, 1, 32, 1), ("f32", 64, 31, 1, 16, 1),
 ])
 def test_attend(gpu_device, lens, dtype, dim, hq, hkv, page, rows):
     c = Case(gpu_device, lens, dtype=dtype, dim=dim, hq=hq, hkv=hkv, page=page, rows=rows)
