@@ -62,27 +62,62 @@ __device__ __forceinline__ bool same_above(uint32_t key, uint32_t prefix, int k)
 // What a selection has found: tokens with keys above `key` stay, and the first `ties` of those equal to it; or (all) every key >= key.
 struct Selected { uint32_t key; int ties; int all; };
 
-// A step's bin, from the histogram in LDS (bin b at count(b)): the one in which the rank-th largest key lies. Whole workgroup.
-template <class Count>
-__device__ __forceinline__ void pick_bin(Count count, int step, uint32_t& prefix, int& rank, bool& all) {
-  __shared__ int s_sum[EV_W], s_bin, s_left, s_all;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  // thread t: the two bins 2047 - 2 t and 2046 - 2 t
-  const int c0 = count(EV_BINS - 1 - 2 * tid), c1 = count(EV_BINS - 2 - 2 * tid);
-  const int incl = wave_scan_i32(c0 + c1);
-  if (lane == 63) s_sum[wave] = incl;
-  __syncthreads();
-  int before = incl - c0 - c1;
+// A step's bin, from the histogram in LDS: the one in which the rank-th largest key lies. The first wavefront looks, a lane at 32 bins from the top, then
+// at the bins of the lane that has it; the whole workgroup calls, behind a barrier. (Two bins a thread and a scan over the workgroup: 1.6 us, this: TIMES.)
+struct Picked { int bin, left, all; };
+__device__ __forceinline__ void pick_bin(const int* hist, int step, Picked* s_pick, uint32_t& prefix, int& rank, bool& all) {
+  const int lane = threadIdx.x & 63;
+  if (threadIdx.x < 64) {
+    const int top = EV_BINS - 32 * (lane + 1);     // the lane's bins: top .. top + 31
+    int sum = 0;
 #pragma unroll
-  for (int i = 0; i < EV_W; ++i) before += i < wave ? s_sum[i] : 0;
-  const int left0 = rank - before, left1 = left0 - c0;
-  if (left0 > 0 && left0 <= c0) { s_bin = EV_BINS - 1 - 2 * tid; s_left = left0; s_all = left0 == c0; }
-  else if (left1 > 0 && left1 <= c1) { s_bin = EV_BINS - 2 - 2 * tid; s_left = left1; s_all = left1 == c1; }
+    for (int i = 0; i < 8; ++i) {                  // (each lane begins elsewhere: other banks)
+      const int4 c = *(const int4*)&hist[top + 4 * ((lane + i) & 7)];
+      sum += (c.x + c.y) + (c.z + c.w);
+    }
+    const int incl = wave_scan_i32(sum);
+    const unsigned long long has = __ballot(incl >= rank);
+    const int l = (int)__builtin_ctzll(has), left = rank - (__shfl(incl, l, 64) - __shfl(sum, l, 64));
+    const int bin = EV_BINS - 32 * l - 1 - min(lane, 31), c = lane < 32 ? hist[bin] : 0;
+    const int seen = wave_scan_i32(c);
+    const unsigned long long in = __ballot(seen >= left);
+    if (lane == (int)__builtin_ctzll(in)) *s_pick = Picked{bin, left - (seen - c), seen == left};
+  }
   __syncthreads();
-  prefix |= (uint32_t)s_bin << digit_shift(step);
-  rank = s_left;
-  all = s_all != 0;                               // the whole bin stays: no need to look into it
-  __syncthreads();
+  const Picked p = *s_pick;
+  prefix |= (uint32_t)p.bin << digit_shift(step);
+  rank = p.left;
+  all = p.all != 0;                               // the whole bin stays: no need to look into it
+}
+
+// The keys of PER tokens at first, first + stride, ..., below n (others: 0): places, then marks, all on their way together. bad: a page is not in the pool.
+template <int PER>
+__device__ __forceinline__ void load_keys(const PagedCall& a, int s, int h, int n, int first, int stride, int count, uint32_t (&key)[PER], bool& bad) {
+  const PagedDims& D = a.D;
+  const int32_t* table = a.table + (size_t)s * D.table_pages;
+  const int seen = a.seen[s];
+  constexpr int AT_ONCE = PER < 16 ? PER : 16;
+#pragma unroll
+  for (int e0 = 0; e0 < PER; e0 += AT_ONCE) {
+#pragma unroll
+    for (int e = 0; e < AT_ONCE; ++e) key[e0 + e] = 0u;
+    if (e0 >= count) continue;                     // (uniform)
+    int page[AT_ONCE], pos[AT_ONCE];
+    float w[AT_ONCE];
+#pragma unroll
+    for (int e = 0; e < AT_ONCE; ++e) page[e] = table[min(first + (e0 + e) * stride, n - 1) >> D.page_shift];
+#pragma unroll
+    for (int e = 0; e < AT_ONCE; ++e) {
+      const bool good = (unsigned)page[e] < (unsigned)D.n_pages;
+      bad |= !good;
+      const size_t mark = paged_mark(D, good ? page[e] : 0, h, min(first + (e0 + e) * stride, n - 1));
+      pos[e] = a.pos[mark];
+      w[e] = a.weight[mark];
+    }
+#pragma unroll
+    for (int e = 0; e < AT_ONCE; ++e)
+      if (first + (e0 + e) * stride < n) key[e0 + e] = evict_key(a, pos[e], w[e], seen);
+  }
 }
 
 // Tiles of scratch in front of a sequence (each (sequence, KV head) has PAGED_TILE entries a tile).
@@ -149,41 +184,30 @@ template <int PER, bool FEW>
 __global__ __launch_bounds__(EV_T) void paged_select_kernel(PagedCall a) {
   const PagedDims& D = a.D;
   const int s = blockIdx.y, h = blockIdx.x, slot = s * D.Hkv + h, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  constexpr int COPIES = 4;                       // of the histogram, by lane: equal digits of a wavefront meet less often
-  __shared__ __align__(16) int hist[EV_BINS * COPIES];
+  __shared__ __align__(16) int hist[3][EV_BINS];  // one for each step, cleared together
+  __shared__ Picked s_pick[3];
   __shared__ int s_count[3][EV_W], s_bad;
   __shared__ int s_to[FEW ? EV_FEW : 1], s_from[FEW ? EV_FEW : 1];
   const int n = paged_len(a, s), keep = a.keep;
   if (!FEW && tid == 0) a.move_head[2 * slot + 1] = 0;
   if (n <= keep) return;
   if (tid == 0) s_bad = 0;
-  const int per = (n + EV_T - 1) / EV_T, base = wave * 64 * per + lane, seen = a.seen[s];
-  const int32_t* table = a.table + (size_t)s * D.table_pages;
+  for (int b = tid; b < 3 * EV_BINS; b += EV_T) ((int*)hist)[b] = 0;
+  const int per = (n + EV_T - 1) / EV_T, base = wave * 64 * per + lane;
   uint32_t key[PER];
   bool bad = false;
-#pragma unroll
-  for (int e = 0; e < PER; ++e) {
-    key[e] = 0u;
-    if (e >= per) continue;
-    const int i = min(base + 64 * e, n - 1), page = table[i >> D.page_shift];
-    const bool good = (unsigned)page < (unsigned)D.n_pages;
-    bad |= !good;
-    const size_t mark = paged_mark(D, good ? page : 0, h, i);
-    key[e] = evict_key(a, a.pos[mark], a.weight[mark], seen);
-  }
+  load_keys(a, s, h, n, base, 64, per, key, bad);
   __syncthreads();
   if (bad) s_bad = 1;
   uint32_t prefix = 0u;
   int rank = keep;
   bool all = false;
   for (int step = 0; step < 3 && !all; ++step) {
-    for (int b = tid; b < EV_BINS * COPIES; b += EV_T) hist[b] = 0;
-    __syncthreads();
 #pragma unroll
     for (int e = 0; e < PER; ++e)
-      if (e < per && base + 64 * e < n && same_above(key[e], prefix, step)) atomicAdd(&hist[digit_of(key[e], step) * COPIES + lane % COPIES], 1);
+      if (e < per && base + 64 * e < n && same_above(key[e], prefix, step)) atomicAdd(&hist[step][digit_of(key[e], step)], 1);
     __syncthreads();
-    pick_bin([&](int b) { const int4 c = *(const int4*)&hist[b * COPIES]; return c.x + c.y + c.z + c.w; }, step, prefix, rank, all);
+    pick_bin(hist[step], step, &s_pick[step], prefix, rank, all);
   }
   if (s_bad) {                                    // (left as it is)
     if (tid == 0) atomicCAS(a.err, 0, LTRI_EINVAL);
@@ -316,26 +340,22 @@ __global__ __launch_bounds__(EV_T) void paged_long_keys_kernel(PagedCall a) {
     return;
   }
   if (first >= n) return;
-  __shared__ int hist[EV_BINS];
+  __shared__ __align__(16) int hist[EV_BINS];
+  __shared__ Picked s_pick;
   for (int b = tid; b < EV_BINS; b += EV_T) hist[b] = 0;
   const long long before = list_tiles_before(a, s);
   const bool room = before + paged_tiles(n) <= D.score_tiles;
   const size_t base = list_base(a, before, n, h);
-  const int32_t* table = a.table + (size_t)s * D.table_pages;
-  const int seen = a.seen[s];
   int32_t* state = a.long_state + (size_t)slot * EV_LONG_WORDS;         // [0] ticket, [1] bad pages, [2] candidates, [3] unused, then the histogram
   bool bad = false;
+  uint32_t key[EV_CHUNK / EV_T];
+  load_keys(a, s, h, n, first + tid, EV_T, EV_CHUNK / EV_T, key, bad);
 #pragma unroll
   for (int e = 0; e < EV_CHUNK / EV_T; ++e) {
     const int i = first + e * EV_T + tid;
     if (i >= n) continue;
-    const int page = table[i >> D.page_shift];
-    const bool good = (unsigned)page < (unsigned)D.n_pages;
-    bad |= !good;
-    const size_t mark = paged_mark(D, good ? page : 0, h, i);
-    const uint32_t k = evict_key(a, a.pos[mark], a.weight[mark], seen);
-    if (room) a.keys[base + i] = k;
-    atomicAdd(&hist[digit_of(k, 0)], 1);
+    if (room) a.keys[base + i] = key[e];
+    atomicAdd(&hist[digit_of(key[e], 0)], 1);
   }
   if (bad) { atomicOr(state + 1, 1); atomicCAS(a.err, 0, LTRI_EINVAL); }
   __syncthreads();
@@ -350,7 +370,7 @@ __global__ __launch_bounds__(EV_T) void paged_long_keys_kernel(PagedCall a) {
   uint32_t prefix = 0u;
   int rank = a.keep;
   bool all = false;
-  pick_bin([&](int b) { return hist[b]; }, 0, prefix, rank, all);
+  pick_bin(hist, 0, &s_pick, prefix, rank, all);
   if (tid == 0) {
     const bool live = room && !__hip_atomic_load(state + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (!room) atomicCAS(a.err, 0, LTRI_ECAPACITY);
@@ -372,7 +392,8 @@ __global__ __launch_bounds__(EV_T) void paged_long_select_kernel(PagedCall a) {
   const uint32_t* keys = (const uint32_t*)a.keys + L->base;
   uint32_t* found = (uint32_t*)a.candidates + L->base;
   int32_t* state = a.long_state + (size_t)slot * EV_LONG_WORDS;
-  __shared__ int hist[EV_BINS];
+  __shared__ __align__(16) int hist[EV_BINS];
+  __shared__ Picked s_pick;
   __shared__ int s_n, s_at;
   if (tid == 0) s_n = 0;
   __syncthreads();
@@ -413,7 +434,7 @@ __global__ __launch_bounds__(EV_T) void paged_long_select_kernel(PagedCall a) {
         if (i0 + e * EV_T + tid < m && same_above(k[e], prefix, step)) atomicAdd(&hist[digit_of(k[e], step)], 1);
     }
     __syncthreads();
-    pick_bin([&](int b) { return hist[b]; }, step, prefix, rank, all);
+    pick_bin(hist, step, &s_pick, prefix, rank, all);
   }
   if (tid == 0) {
     state[2] = 0;
@@ -543,7 +564,7 @@ template <bool FEW>
 static void launch_select(const PagedCall& a, hipStream_t s) {
   const dim3 grid(a.D.Hkv, a.seq_count);
   if (a.D.cap_tokens <= 4 * EV_T) paged_select_kernel<4, FEW><<<grid, EV_T, 0, s>>>(a);
-  else if (a.D.cap_tokens <= 16 * EV_T) paged_select_kernel<16, FEW><<<grid, EV_T, 0, s>>>(a);
+  else if (a.D.cap_tokens <= 8 * EV_T) paged_select_kernel<8, FEW><<<grid, EV_T, 0, s>>>(a);
   else paged_select_kernel<EV_LONG / EV_T, FEW><<<grid, EV_T, 0, s>>>(a);
 }
 

@@ -17,7 +17,7 @@ constexpr int PAGED_SCORE_PAIRS = 31;
 __host__ __device__ constexpr bool paged_keeps_scores(int pairs) { return pairs <= PAGED_SCORE_PAIRS; }
 
 // Eviction: tables of up to EV_LONG tokens are selected from by one workgroup per (sequence, KV head), longer ones by several.
-constexpr int EV_LONG = 32768, EV_CHUNK = 8192;
+constexpr int EV_LONG = 16384, EV_CHUNK = 8192;
 constexpr int EV_LONG_WORDS = 4 + 2048;    // counters of a (sequence, KV head), zero between launches
 constexpr int EV_SLOT_BYTES = 24;          // what the launches of a long selection tell each other
 

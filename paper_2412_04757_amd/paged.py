@@ -38,6 +38,7 @@ class LtriPagedCache:
         self.dry = dry
         self.cfg = cfg = LtriPagedConfig.from_buffer_copy(cfg)
         self.tdtype = torch.float32 if cfg.dtype == LTRI_F32 else torch.bfloat16
+        self._index = -1                                     # of the device, as tensors say it (-1: the CPU)
         shape = (cfg.n_pages, cfg.n_kv_heads, cfg.page_tokens, cfg.head_dim)
         if (k_pages is None) != (v_pages is None):
             raise ValueError("k_pages and v_pages: both or neither")
@@ -56,6 +57,7 @@ class LtriPagedCache:
             self._check(self.lib.ltri_paged_create_dry(C.byref(cfg), C.byref(self.handle)))
             return
         self.device = device = torch.device(device.type, torch.cuda.current_device() if device.index is None else device.index)
+        self._index = device.index
         with torch.cuda.device(device):
             if k_pages is None:
                 k_pages = torch.zeros(shape, dtype=self.tdtype, device=device)
@@ -97,18 +99,17 @@ class LtriPagedCache:
         except Exception:
             pass
 
-    def _arg(self, name: str, t: Optional[torch.Tensor], shape, dtype: torch.dtype) -> Optional[int]:
-        """Address of a dense tensor of this shape on the cache's device."""
-        if t is None or not isinstance(t, torch.Tensor):     # (a stand-in with an address: dry caches in the host tests)
-            return _ptr(t)
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-        if not self.dry and t.device != self.device:
-            raise ValueError(f"{name} is on {t.device}, the cache on {self.device}")
-        return _ptr(t, dtype)
+    def _arg(self, name: str, t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype) -> Optional[int]:
+        """Address of a dense tensor of this shape on the cache's device. (A decoding step is as long as a few of these calls: one condition.)"""
+        if t is None:
+            return None
+        if t.shape != shape or t.dtype is not dtype or not t.is_contiguous() or t.get_device() != self._index:
+            raise ValueError(f"{name}: expected a dense {dtype} {shape} on {'the CPU' if self.dry else self.device}; got {t.dtype} "
+                             f"{tuple(t.shape)}, strides {tuple(t.stride())}, on {t.device}")
+        return t.data_ptr()
 
     def _places(self, table, lens, seen=None):
-        n = table.shape[0]
+        n = len(table)
         return (n, self._arg("table", table, (n, self.cfg.table_pages), torch.int32), self._arg("lens", lens, (n,), torch.int32),
                 self._arg("seen", seen, (n,), torch.int32))
 
@@ -122,7 +123,7 @@ class LtriPagedCache:
         shape = (n, n_q, c.n_q_heads, c.head_dim)
         q_ptr = self._arg("q", q, shape, self.tdtype)
         if out is None:
-            out = torch.empty(shape, dtype=self.tdtype, device=q.device)
+            out = torch.empty_like(q)
         return q_ptr, n_q, out, self._arg("out", out, shape, self.tdtype), self._arg("lse", lse, shape[:3], torch.float32)
 
     # ---- the C ABI, same names ----
