@@ -75,9 +75,15 @@ __device__ __forceinline__ float second_float(unsigned long long v) { return __u
 __device__ __forceinline__ float safe_ref(float m) { return m == -INFINITY ? 0.f : m; }
 
 // A wavefront's matrix products of one tile, by type. NU: groups of 16 tokens in a tile; VW: 32-bit words of a lane's piece of a value row.
-template <int DT, int DIM> struct TileOps;
+// ONCE: no other wavefront reads these rows: they pass the caches by. 16 x 128K tokens 1394 -> 1268 us, 64 ragged sequences 193 -> 180; where wavefronts share
+// rows (16 query rows over 32K) it is 59 -> 85.
+template <bool ONCE, class T> __device__ __forceinline__ T load_row(const char* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load((const T*)p);
+  else return *(const T*)p;
+}
+template <int DT, int DIM, bool ONCE> struct TileOps;
 
-template <int DIM> struct TileOps<LTRI_BF16, DIM> {
+template <int DIM, bool ONCE> struct TileOps<LTRI_BF16, DIM, ONCE> {
   static constexpr int NU = 2, NK = DIM / 32, NT = DIM / 16, CP = NT, VW = CP / 2;
   typedef u32x4_t Piece;
   Piece q[NK], k[NU][NK];
@@ -89,15 +95,15 @@ template <int DIM> struct TileOps<LTRI_BF16, DIM> {
   }
   __device__ __forceinline__ void load_k(int u, const char* row, int g) {            // row: of token 16 u + lane % 16
 #pragma unroll
-    for (int i = 0; i < NK; ++i) k[u][i] = *(const u32x4_t*)(row + i * 64 + g * 16);
+    for (int i = 0; i < NK; ++i) k[u][i] = load_row<ONCE, u32x4_t>(row + i * 64 + g * 16);
   }
   __device__ __forceinline__ void store_k(int u, char* row, int g) const {
 #pragma unroll
     for (int i = 0; i < NK; ++i) *(u32x4_t*)(row + i * 64 + g * 16) = k[u][i];
   }
   __device__ __forceinline__ void load_v(int u, int j, const char* row, int kl) {    // row: of token 16 u + 4 (lane / 16) + j
-    if constexpr (VW == 4) { const u32x4_t x = *(const u32x4_t*)(row + kl * 16); v[u][j][0] = x[0]; v[u][j][1] = x[1]; v[u][j][2] = x[2]; v[u][j][3] = x[3]; }
-    else { const u32x2_t x = *(const u32x2_t*)(row + kl * 8); v[u][j][0] = x[0]; v[u][j][1] = x[1]; }
+    if constexpr (VW == 4) { const u32x4_t x = load_row<ONCE, u32x4_t>(row + kl * 16); v[u][j][0] = x[0]; v[u][j][1] = x[1]; v[u][j][2] = x[2]; v[u][j][3] = x[3]; }
+    else { const u32x2_t x = load_row<ONCE, u32x2_t>(row + kl * 8); v[u][j][0] = x[0]; v[u][j][1] = x[1]; }
   }
   __device__ __forceinline__ void store_v(int u, int j, char* row, int kl) const {
     if constexpr (VW == 4) *(u32x4_t*)(row + kl * 16) = u32x4_t{v[u][j][0], v[u][j][1], v[u][j][2], v[u][j][3]};
@@ -159,7 +165,7 @@ template <int DIM> struct TileOps<LTRI_BF16, DIM> {
   }
 };
 
-template <int DIM> struct TileOps<LTRI_F32, DIM> {
+template <int DIM, bool ONCE> struct TileOps<LTRI_F32, DIM, ONCE> {
   static constexpr int NU = 1, NK = DIM / 16, NT = DIM / 16, CP = 4, VW = DIM / 16;
   typedef f32x4_t Piece;
   Piece q[NK], k[NU][NK];
@@ -171,7 +177,7 @@ template <int DIM> struct TileOps<LTRI_F32, DIM> {
   }
   __device__ __forceinline__ void load_k(int u, const char* row, int g) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) k[u][i] = *(const f32x4_t*)(row + i * 64 + g * 16);
+    for (int i = 0; i < NK; ++i) k[u][i] = load_row<ONCE, f32x4_t>(row + i * 64 + g * 16);
   }
   __device__ __forceinline__ void store_k(int u, char* row, int g) const {
 #pragma unroll
@@ -180,7 +186,7 @@ template <int DIM> struct TileOps<LTRI_F32, DIM> {
   __device__ __forceinline__ void load_v(int u, int j, const char* row, int kl) {
 #pragma unroll
     for (int c = 0; c < VW / 4; ++c) {
-      const u32x4_t x = *(const u32x4_t*)(row + c * 256 + kl * 16);
+      const u32x4_t x = load_row<ONCE, u32x4_t>(row + c * 256 + kl * 16);
       v[u][j][4 * c] = x[0]; v[u][j][4 * c + 1] = x[1]; v[u][j][4 * c + 2] = x[2]; v[u][j][4 * c + 3] = x[3];
     }
   }
@@ -279,7 +285,7 @@ __device__ __forceinline__ void write_result(const PagedCall& a, size_t r, int c
 // SMALL: pages of fewer than 16 tokens, whose page is looked up lane by lane; else a group of 16 tokens lies in one page.
 template <int DT, int DIM, int WB, bool SMALL>
 __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCall a, int min_share, int merge_later) {
-  typedef TileOps<DT, DIM> Ops;
+  typedef TileOps<DT, DIM, WB == 1> Ops;
   constexpr int T = PagedTile<DT>::N, NU = Ops::NU, NT = Ops::NT, CP = Ops::CP, ELT = DT == LTRI_F32 ? 4 : 2;
   constexpr int PITCH = DIM + 4;
   static_assert(NU * 16 == T && WALK_T == 64 * PA_WAVES, "");
@@ -737,7 +743,7 @@ __global__ __launch_bounds__(WALK_T) void paged_weights_kernel(PagedCall a) {
 template <int DT, int DIM>
 __global__ __launch_bounds__(WALK_T, 2) void paged_key_weights_kernel(PagedCall a) {
   constexpr int T = PagedTile<DT>::N, ELT = DT == LTRI_F32 ? 4 : 2, WAVES = WALK_T / 64, NB = 4;
-  typedef TileOps<DT, DIM> Ops;
+  typedef TileOps<DT, DIM, true> Ops;
   constexpr int NU = Ops::NU;
   const PagedDims& D = a.D;
   const int pairs = a.n * D.G, w = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kl = lane & 15, g = lane >> 4;
