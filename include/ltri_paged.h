@@ -28,8 +28,8 @@
  * Sequences may share pages for reading. Where a call writes (appended rows, weights, evictions), the written tokens'
  * pages belong to one sequence of the call only, and with weights no page is named twice in a call.
  *
- * Conventions are those of ltri.h: statuses, caller-owned buffers, work enqueued on the handle's stream without
- * waiting. A call runs on the device that was current at creation, whatever is current when it is made. Calls on one
+ * Conventions are those of ltri.h: statuses, caller-owned buffers (alive until the work on them is done), work enqueued on
+ * the handle's stream without waiting. A call runs on the device that was current at creation, whatever is current when it is made. Calls on one
  * handle must not overlap; handles may share a scratch buffer if their calls do not overlap. k/v pages and rows, q and
  * out are 16-byte aligned (EINVAL else). What only the device can see is reported by ltri_paged_sync_status(): a length
  * beyond the table's capacity (LTRI_ECAPACITY; the sequence is taken as length 0) and a page outside [0, n_pages)
@@ -50,7 +50,7 @@ extern "C" {
 typedef struct ltri_paged ltri_paged;
 
 typedef struct {
-  int32_t n_q_heads, n_kv_heads, head_dim;   /* head_dim 64 or 128; up to 128 query heads per KV head */
+  int32_t n_q_heads, n_kv_heads, head_dim;   /* head_dim 64 or 128; at most 4096 query heads, 128 per KV head */
   int32_t dtype;                             /* LTRI_F32 | LTRI_BF16                       */
   int32_t page_tokens;                       /* a power of two, 1 to 4096                  */
   int32_t n_pages;                           /* pages in the pool                          */

@@ -33,7 +33,7 @@ static size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 static int32_t derive(const ltri_paged_config* cfg, PagedDims& D, PagedLayout& L) {
   if (!cfg) return LTRI_EINVAL;
   const ltri_paged_config& c = *cfg;
-  if (c.n_q_heads < 1 || c.n_kv_heads < 1 || c.n_kv_heads > 65535 || c.n_q_heads % c.n_kv_heads || c.n_q_heads / c.n_kv_heads > 128)
+  if (c.n_q_heads < 1 || c.n_q_heads > 4096 || c.n_kv_heads < 1 || c.n_q_heads % c.n_kv_heads || c.n_q_heads / c.n_kv_heads > 128)
     return LTRI_EINVAL;
   if (c.head_dim != 64 && c.head_dim != 128) return LTRI_EINVAL;
   if (c.dtype != LTRI_F32 && c.dtype != LTRI_BF16) return LTRI_EINVAL;

@@ -341,8 +341,9 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
     const int pair = min(pair0 + kl, pairs - 1), query_row = pair / D.G;
     const int sees = len - a.n + 1 + query_row;                      // tokens that the lane's pair sees
     const int all_see = len - a.n + 1 + min(pair0, pairs - 1) / D.G; // ... that every pair of the block sees
-    // tiles from here on: some token is not seen by some pair, or comes with the call (SMALL: every tile takes that way)
-    const int first_edge = SMALL ? t0 : max(0, min(all_see, first_new)) / T;
+    // Tiles from here on: some token is not seen by some pair, or comes with the call. They take a way of their own, without the next
+    // tile's rows on theirs; with SMALL pages every tile does, and has them.
+    const int edge = SMALL ? t0 : min(t1, max(0, min(all_see, first_new)) / T);
     const int32_t* table = a.table + (size_t)s * D.table_pages;
     const char* kh = a.k + (size_t)h * D.head_stride * ELT;
     const char* vh = a.v + (size_t)h * D.head_stride * ELT;
@@ -385,8 +386,8 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
       i = min(i, len - 1);                                           // (the page is that of this token, too)
       return i >= first_new ? new_row(rows, i) : row(base, page, i);
     };
-    auto load_k = [&](int t, const Pages& p) __attribute__((always_inline)) {
-      if (t >= first_edge) {
+    auto load_k = [&](int t, const Pages& p, auto edge_c) __attribute__((always_inline)) {
+      if constexpr (decltype(edge_c)::value) {
         const int kl_ = only_here(kl), g_ = only_here(g);
 #pragma unroll
         for (int u = 0; u < NU; ++u) ops.load_k(u, edge_row(kh, a.k_new, p.k[u], t * T + 16 * u + kl_), g_);
@@ -395,8 +396,8 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
         for (int u = 0; u < NU; ++u) ops.load_k(u, row(kh, p.k[u], t * T + 16 * u) + k_off, 0);
       }
     };
-    auto load_v = [&](int t, const Pages& p) __attribute__((always_inline)) {
-      if (t >= first_edge) {
+    auto load_v = [&](int t, const Pages& p, auto edge_c) __attribute__((always_inline)) {
+      if constexpr (decltype(edge_c)::value) {
         const int kl_ = only_here(kl), g_ = only_here(g);
 #pragma unroll
         for (int u = 0; u < NU; ++u)
@@ -411,9 +412,14 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
     };
 
     Pages now, next;
-    // One tile; EDGE: see first_edge.
+    // One tile; EDGE: see `edge`.
     auto tile = [&](int t, auto edge_c) __attribute__((always_inline)) {
-      constexpr bool EDGE = decltype(edge_c)::value;
+      constexpr bool EDGE = decltype(edge_c)::value, AHEAD = SMALL || !EDGE;
+      if constexpr (!AHEAD) {
+        look_up(t, now);
+        load_k(t, now, edge_c);
+        load_v(t, now, edge_c);
+      }
       f32x4_t sv[NU];
       const int kl_ = EDGE ? only_here(kl) : kl, g_ = EDGE ? only_here(g) : g;
       const bool writes = EDGE && a.k_new && pb == 0 && wave % WB == 0;
@@ -432,11 +438,13 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
           }
         }
       }
-      const bool more = t + STEP < t1;
+      const bool more = AHEAD && t + STEP < (SMALL ? t1 : edge);
       Pages after;
-      look_up(min(t + 2 * STEP, nt - 1), after);
-      if (more) load_k(t + STEP, next);
-      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (AHEAD) {
+        look_up(min(t + 2 * STEP, nt - 1), after);
+        if (more) load_k(t + STEP, next, edge_c);
+        __builtin_amdgcn_sched_barrier(0);
+      }
 
       // of the lane's tokens 16 u + 4 g + j (bit 4 u + j): which are there at all, and which its pair sees
       uint32_t there = 0xFFu, vis = 0xFFu;
@@ -529,23 +537,27 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
         }
       }
       if (!apart) ops.template values<false>(sv, 0u, true);
-      __builtin_amdgcn_sched_barrier(0);
-      if (more) load_v(t + STEP, next);
-      __builtin_amdgcn_sched_barrier(0);
-      now = next;
-      next = after;
+      if constexpr (AHEAD) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) load_v(t + STEP, next, edge_c);
+        __builtin_amdgcn_sched_barrier(0);
+        now = next;
+        next = after;
+      }
     };
     int t = t0 + wave / WB;
     if (pair0 >= pairs) t = t1;                                      // a block without pairs
-    if (t < t1) {
+    if (t < (SMALL ? t1 : edge)) {
+      constexpr std::integral_constant<bool, SMALL> small_c{};
       look_up(t, now);
       look_up(min(t + STEP, nt - 1), next);
-      load_k(t, now);
+      load_k(t, now, small_c);
       __builtin_amdgcn_sched_barrier(0);                             // keys before values, as in the loop: what is waited for first comes first
-      load_v(t, now);
+      load_v(t, now, small_c);
       __builtin_amdgcn_sched_barrier(0);
     }
-    for (; t < min(t1, first_edge); t += STEP) tile(t, std::false_type{});
+    if constexpr (!SMALL)
+      for (; t < edge; t += STEP) tile(t, std::false_type{});
     for (; t < t1; t += STEP) tile(t, std::true_type{});
 
     // the wavefronts' results: own maximum, sum and O

@@ -54,18 +54,30 @@ __device__ __forceinline__ int mask_rank(unsigned long long m) {           // se
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
 }
 
-// Digits of a key from the top: width and shift of step k.
-__device__ __forceinline__ int digit_shift(int k) { return k == 0 ? 21 : k == 1 ? 10 : 0; }
-__device__ __forceinline__ uint32_t digit_of(uint32_t key, int k) { return k == 2 ? key & 1023u : (key >> digit_shift(k)) & 2047u; }
-__device__ __forceinline__ bool same_above(uint32_t key, uint32_t prefix, int k) { return k == 0 || ((key ^ prefix) >> digit_shift(k - 1)) == 0; }
+// Digits of a key from the top: shift and value of step K.
+constexpr int digit_shift(int k) { return k == 0 ? 21 : k == 1 ? 10 : 0; }
+template <int K> __device__ __forceinline__ uint32_t digit_of(uint32_t key) { return K == 2 ? key & 1023u : (key >> digit_shift(K)) & 2047u; }
+template <int K> __device__ __forceinline__ bool same_above(uint32_t key, uint32_t prefix) {
+  if constexpr (K == 0) return true;
+  else return ((key ^ prefix) >> digit_shift(K - 1)) == 0;
+}
+template <int K> using Step = std::integral_constant<int, K>;
 
-// What a selection has found: tokens with keys above `key` stay, and the first `ties` of those equal to it; or (all) every key >= key.
-struct Selected { uint32_t key; int ties; int all; };
+// Counts a key in a step's histogram, whole wavefronts (`in`: the lane has one). Protected tokens, which share a bin, as one addition.
+template <int K>
+__device__ __forceinline__ void count_key(int* hist, uint32_t key, bool in, uint32_t prefix) {
+  in = in && same_above<K>(key, prefix);
+  const bool top = in && key == 0xFFFFFFFFu;
+  const unsigned long long m = __ballot(top);
+  if (m && (threadIdx.x & 63) == 0) atomicAdd(&hist[digit_of<K>(0xFFFFFFFFu)], __popcll(m));
+  if (in && !top) atomicAdd(&hist[digit_of<K>(key)], 1);
+}
 
 // A step's bin, from the histogram in LDS: the one in which the rank-th largest key lies. The first wavefront looks, a lane at 32 bins from the top, then
-// at the bins of the lane that has it; the whole workgroup calls, behind a barrier. (Two bins a thread and a scan over the workgroup: 1.6 us, this: TIMES.)
+// at the bins of the lane that has it; the whole workgroup calls, behind a barrier. (Two bins a thread and a scan over the workgroup: 1.6 us, this: 0.8.)
 struct Picked { int bin, left, all; };
-__device__ __forceinline__ void pick_bin(const int* hist, int step, Picked* s_pick, uint32_t& prefix, int& rank, bool& all) {
+template <int K>
+__device__ __forceinline__ void pick_bin(const int* hist, Picked* s_pick, uint32_t& prefix, int& rank, bool& all) {
   const int lane = threadIdx.x & 63;
   if (threadIdx.x < 64) {
     const int top = EV_BINS - 32 * (lane + 1);     // the lane's bins: top .. top + 31
@@ -85,7 +97,7 @@ __device__ __forceinline__ void pick_bin(const int* hist, int step, Picked* s_pi
   }
   __syncthreads();
   const Picked p = *s_pick;
-  prefix |= (uint32_t)p.bin << digit_shift(step);
+  prefix |= (uint32_t)p.bin << digit_shift(K);
   rank = p.left;
   all = p.all != 0;                               // the whole bin stays: no need to look into it
 }
@@ -120,18 +132,11 @@ __device__ __forceinline__ void load_keys(const PagedCall& a, int s, int h, int 
   }
 }
 
-// Tiles of scratch in front of a sequence (each (sequence, KV head) has PAGED_TILE entries a tile).
+// Tiles of scratch in front of a sequence (each (sequence, KV head) has PAGED_TILE entries a tile); every wavefront adds for itself.
 __device__ __forceinline__ long long list_tiles_before(const PagedCall& a, int s) {
-  __shared__ unsigned long long s_before;
-  if (threadIdx.x == 0) s_before = 0;
-  __syncthreads();
   unsigned long long tiles = 0;
-  for (int i = threadIdx.x; i < s; i += EV_T) tiles += (unsigned long long)paged_tiles(paged_len(a, i));
-  if (tiles) atomicAdd(&s_before, tiles);
-  __syncthreads();
-  const long long r = (long long)s_before;
-  __syncthreads();
-  return r;
+  for (int i = threadIdx.x & 63; i < s; i += 64) tiles += (unsigned long long)paged_tiles(paged_len(a, i));
+  return __shfl((long long)wave_scan_u64(tiles), 63, 64);
 }
 __device__ __forceinline__ size_t list_base(const PagedCall& a, long long before, int n, int h) {
   return ((size_t)before * a.D.Hkv + (size_t)h * paged_tiles(n)) * PAGED_TILE;
@@ -202,13 +207,18 @@ __global__ __launch_bounds__(EV_T) void paged_select_kernel(PagedCall a) {
   uint32_t prefix = 0u;
   int rank = keep;
   bool all = false;
-  for (int step = 0; step < 3 && !all; ++step) {
+  auto step = [&](auto k) __attribute__((always_inline)) {
+    constexpr int K = decltype(k)::value;
+    if (all) return;
 #pragma unroll
     for (int e = 0; e < PER; ++e)
-      if (e < per && base + 64 * e < n && same_above(key[e], prefix, step)) atomicAdd(&hist[step][digit_of(key[e], step)], 1);
+      if (e < per) count_key<K>(hist[K], key[e], base + 64 * e < n, prefix);
     __syncthreads();
-    pick_bin(hist[step], step, &s_pick[step], prefix, rank, all);
-  }
+    pick_bin<K>(hist[K], &s_pick[K], prefix, rank, all);
+  };
+  step(Step<0>{});
+  step(Step<1>{});
+  step(Step<2>{});
   if (s_bad) {                                    // (left as it is)
     if (tid == 0) atomicCAS(a.err, 0, LTRI_EINVAL);
     if constexpr (!FEW) return;
@@ -225,7 +235,8 @@ __global__ __launch_bounds__(EV_T) void paged_select_kernel(PagedCall a) {
     for (int i = 0; i < EV_W; ++i) ties += i < wave ? s_count[0][i] : 0;
   }
   // bits of the lane's tokens that stay
-  uint64_t stays = 0ull;
+  static_assert(PER <= 32, "");
+  uint32_t stays = 0u;
   int holes = 0, comers = 0;
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
@@ -238,7 +249,7 @@ __global__ __launch_bounds__(EV_T) void paged_select_kernel(PagedCall a) {
       stay |= tie && ties + mask_rank(m) < rank;
       ties += __popcll(m);
     }
-    stays |= (uint64_t)stay << e;
+    stays |= (uint32_t)stay << e;
     holes += __popcll(__ballot(i < keep && !stay));
     comers += __popcll(__ballot(i >= keep && stay));
   }
@@ -308,7 +319,7 @@ __global__ __launch_bounds__(256) void paged_move_kernel(PagedCall a) {
 
 struct LongSlot {                                  // of a (sequence, KV head)
   long long base;                                  // of its keys, candidates and moves in scratch
-  uint32_t key; int ties, all;                     // Selected; after launch 1 the bin's prefix and the rank in it
+  uint32_t key; int ties, all;                     // keys above `key` stay and the first `ties` equal to it, or (all) those >= key; after launch 1: of the bin
   int live;                                        // 0: nothing to do
 };
 static_assert(sizeof(LongSlot) == EV_SLOT_BYTES, "");
@@ -350,12 +361,12 @@ __global__ __launch_bounds__(EV_T) void paged_long_keys_kernel(PagedCall a) {
   bool bad = false;
   uint32_t key[EV_CHUNK / EV_T];
   load_keys(a, s, h, n, first + tid, EV_T, EV_CHUNK / EV_T, key, bad);
+  __syncthreads();
 #pragma unroll
   for (int e = 0; e < EV_CHUNK / EV_T; ++e) {
     const int i = first + e * EV_T + tid;
-    if (i >= n) continue;
-    if (room) a.keys[base + i] = key[e];
-    atomicAdd(&hist[digit_of(key[e], 0)], 1);
+    if (room && i < n) a.keys[base + i] = key[e];
+    count_key<0>(hist, key[e], i < n, 0u);
   }
   if (bad) { atomicOr(state + 1, 1); atomicCAS(a.err, 0, LTRI_EINVAL); }
   __syncthreads();
@@ -370,7 +381,7 @@ __global__ __launch_bounds__(EV_T) void paged_long_keys_kernel(PagedCall a) {
   uint32_t prefix = 0u;
   int rank = a.keep;
   bool all = false;
-  pick_bin(hist, 0, &s_pick, prefix, rank, all);
+  pick_bin<0>(hist, &s_pick, prefix, rank, all);
   if (tid == 0) {
     const bool live = room && !__hip_atomic_load(state + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (!room) atomicCAS(a.err, 0, LTRI_ECAPACITY);
@@ -404,7 +415,7 @@ __global__ __launch_bounds__(EV_T) void paged_long_select_kernel(PagedCall a) {
   for (int e = 0; e < EV_CHUNK / EV_T; ++e) {
     const int i = first + e * EV_T + tid;
     key[e] = keys[min(i, n - 1)];
-    mine += i < n && same_above(key[e], prefix, 1);
+    mine += i < n && same_above<1>(key[e], prefix);
   }
   const int incl = wave_scan_i32(mine);
   int at = 0;
@@ -417,12 +428,14 @@ __global__ __launch_bounds__(EV_T) void paged_long_select_kernel(PagedCall a) {
 #pragma unroll
   for (int e = 0; e < EV_CHUNK / EV_T; ++e) {
     const int i = first + e * EV_T + tid;
-    if (i < n && same_above(key[e], prefix, 1)) __hip_atomic_store(found + at++, key[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (i < n && same_above<1>(key[e], prefix)) __hip_atomic_store(found + at++, key[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   if (!last_of(state, (n + EV_CHUNK - 1) / EV_CHUNK)) return;
   const int m = __hip_atomic_load(state + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   bool all = false;
-  for (int step = 1; step < 3 && !all; ++step) {
+  auto step = [&](auto k_c) __attribute__((always_inline)) {
+    constexpr int K = decltype(k_c)::value;
+    if (all) return;
     for (int b = tid; b < EV_BINS; b += EV_T) hist[b] = 0;
     __syncthreads();
     for (int i0 = 0; i0 < m; i0 += 8 * EV_T) {
@@ -430,12 +443,13 @@ __global__ __launch_bounds__(EV_T) void paged_long_select_kernel(PagedCall a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) k[e] = __hip_atomic_load(found + min(i0 + e * EV_T + tid, m - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (i0 + e * EV_T + tid < m && same_above(k[e], prefix, step)) atomicAdd(&hist[digit_of(k[e], step)], 1);
+      for (int e = 0; e < 8; ++e) count_key<K>(hist, k[e], i0 + e * EV_T + tid < m, prefix);
     }
     __syncthreads();
-    pick_bin(hist, step, &s_pick, prefix, rank, all);
-  }
+    pick_bin<K>(hist, &s_pick, prefix, rank, all);
+  };
+  step(Step<1>{});
+  step(Step<2>{});
   if (tid == 0) {
     state[2] = 0;
     L->key = prefix;

@@ -21,6 +21,7 @@ LENS = ([1], [0], [31, 32, 33], [0, 1, 700, 64, 0, 17], [5000], [2049, 3, 128, 1
     ("bf16", 128, 8, 2, 16, 1), ("bf16", 128, 4, 4, 64, 1), ("bf16", 64, 8, 1, 1, 2), ("bf16", 128, 14, 2, 8, 3), ("bf16", 128, 32, 1, 32, 1),
     ("bf16", 64, 6, 2, 256, 16), ("f32", 64, 4, 1, 32, 1), ("f32", 128, 8, 2, 16, 4), ("f32", 128, 3, 3, 128, 1), ("bf16", 128, 8, 2, 2, 5),
     ("f32", 128, 12, 2, 16, 7), ("f32", 64, 10, 2, 4, 6), ("bf16", 128, 10, 2, 64, 6), ("bf16", 64, 31, 1, 32, 1), ("f32", 64, 31, 1, 16, 1),
+    ("bf16", 64, 4, 2, 4096, 2),
 ])
 def test_attend(gpu_device, lens, dtype, dim, hq, hkv, page, rows):
     c = Case(gpu_device, lens, dtype=dtype, dim=dim, hq=hq, hkv=hkv, page=page, rows=rows)
@@ -56,6 +57,44 @@ def test_attend_many_sequences(gpu_device, dtype):
     part = c.cache.attend(c.d_table[100:163], c.d_lens[100:163], c.on(c.q[100:163]))
     want, _ = O.attend(c.k, c.v, None, c.table[100:163], c.lens[100:163], c.q[100:163])
     c.check_attend(part, None, want, None)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sequences_that_share_pages(gpu_device, dtype):
+    """A common beginning, held once: three sequences name its pages, a fourth is one of them again."""
+    c = Case(gpu_device, [160, 500, 97, 160], dtype=dtype, rows=2, weights=False)
+    c.table[1, :6], c.table[2, :6], c.table[3] = c.table[0, :6], c.table[0, :6], c.table[0]
+    c.push()
+    lse = c.new_lse()
+    q = c.on(c.q)
+    q[3], c.q[3] = q[0], c.q[0]
+    out = c.cache.attend(*c.args(False), q, lse=lse)
+    c.check_attend(out, lse, *c.oracle_attend())
+    c.check_pools()
+    assert c.cache.sync_status() == 0
+
+
+def test_weights_of_pages_named_twice_stay_in_bounds(gpu_device):
+    """Weights want every page named once: a batch that holds more tokens than the pool is reported, and nothing but weights is touched."""
+    c = Case(gpu_device, [640] * 12, page=64, spare=0)
+    c.table[1:] = c.table[0]
+    c.push()
+    n_pages = 10
+    cfg = paged_config(c.hq, c.hkv, c.dim, c.dtype, page_tokens=64, n_pages=n_pages, table_pages=10, max_seqs=12, rows_max=1, weights=True)
+    small = [x[torch.from_numpy(c.table[0]).long().to(gpu_device)].contiguous() for x in (c.cache.k_pages, c.cache.v_pages, c.cache.weight, c.cache.pos)]
+    guard = torch.full((1 << 20,), 0xFF, dtype=torch.uint8, device=gpu_device)
+    probe = LtriPagedCache(cfg, gpu_device, k_pages=small[0], v_pages=small[1], weight=small[2], pos=small[3])
+    scratch = torch.cat([torch.full((probe.scratch_bytes,), 0xFF, dtype=torch.uint8, device=gpu_device), guard])
+    cache = LtriPagedCache(cfg, gpu_device, k_pages=small[0], v_pages=small[1], weight=small[2], pos=small[3], scratch=scratch)
+    table = torch.arange(10, dtype=torch.int32, device=gpu_device).repeat(12, 1)
+    out = cache.attend(table, c.d_lens, c.on(c.q), decay=1.0)
+    want, _ = O.attend(c.k, c.v, None, c.table, c.lens, c.q)
+    c.check_attend(out, None, want, None)
+    assert bool((scratch[probe.scratch_bytes:] == 0xFF).all())
+    assert cache.sync_status() == -3
+    cache.evict(table, c.d_lens, c.d_lens.clone(), 100)
+    assert bool((scratch[probe.scratch_bytes:] == 0xFF).all())
+    cache.sync_status()
 
 
 def test_attend_gives_the_same_bits_again(gpu_device):

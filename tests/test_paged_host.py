@@ -24,7 +24,7 @@ def sizes(cfg):
 
 
 @pytest.mark.parametrize("kw", [
-    dict(n_q_heads=7), dict(n_q_heads=0), dict(n_kv_heads=0), dict(n_q_heads=258, n_kv_heads=2), dict(head_dim=96), dict(head_dim=256),
+    dict(n_q_heads=7), dict(n_q_heads=0), dict(n_kv_heads=0), dict(n_q_heads=258, n_kv_heads=2), dict(n_q_heads=4104, n_kv_heads=1026), dict(head_dim=96), dict(head_dim=256),
     dict(page_tokens=0), dict(page_tokens=24), dict(page_tokens=8192), dict(n_pages=0), dict(table_pages=0),
     dict(table_pages=1 << 27), dict(max_seqs=0), dict(max_seqs=4097), dict(rows_max=0), dict(rows_max=65),
     dict(page_stride=2048, head_stride=1024, token_stride=60),            # rows overlap
