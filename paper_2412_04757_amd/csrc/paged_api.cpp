@@ -55,7 +55,8 @@ static int32_t derive(const ltri_paged_config* cfg, PagedDims& D, PagedLayout& L
   } else {
     D.page_stride = c.page_stride; D.head_stride = c.head_stride; D.token_stride = c.token_stride;
     const long long step = 16 / D.elt;
-    struct Axis { long long* stride; long long count; } ax[3] = {{&D.page_stride, c.n_pages}, {&D.head_stride, D.Hkv}, {&D.token_stride, c.page_tokens}};
+    struct Axis { long long* stride; long long count; };
+    Axis ax[3] = {{&D.page_stride, c.n_pages}, {&D.head_stride, D.Hkv}, {&D.token_stride, c.page_tokens}};
     for (const Axis& x : ax) {
       if (x.count == 1) *x.stride = 0;                  // never stepped over, whatever was given
       else if (*x.stride < 1 || *x.stride % step || *x.stride > 1ll << 40) return LTRI_EINVAL;

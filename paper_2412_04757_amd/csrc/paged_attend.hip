@@ -3,18 +3,23 @@
 //
 // What bounds it: the key and value rows, each read once (512 bytes of bf16 rows and 4 G n products of 128 a token and KV head).
 // So nothing is staged: a lane loads 16-byte pieces in the order in which the matrix cores take them, and while a tile of 32
-// tokens (fp32: 16) is used, the next one's rows come into the registers as they fall free; three wavefronts a SIMD hide the rest.
-//   S^T = K Q^T    A = 16 tokens (lane % 16) x head_dim pieces (lane / 16), B = 16 (query row, head) pairs: a lane gets tokens
-//                  4 (lane / 16) + j, j < 4, of pair lane % 16. All query rows and heads of a KV head share the rows that way.
+// tokens (fp32: 16) is used, the next one's rows come into the registers as they fall free: eight wavefronts a compute unit, 128 KB
+// on their way. 16 sequences of 128K tokens, 8 KV heads x 128 in bf16: 1261 us, 6.8 TB/s (a large copy 5.9, a large read 6.9);
+// 2 of 128K in fp32 335 us; one of 1000 tokens 10.8 us, of which the place in the row of tiles takes 1.3, the first rows 3.3, join
+// and partial results 0.8, the ticket 0.9, the merge 3.5 and the launch the rest.
+//   S^T = K Q^T    A = 16 tokens (lane % 16) x head_dim pieces (lane / 16), B = 16 (query row, head) pairs: a lane gets
+//                  tokens 4 (lane / 16) + j, j < 4, of pair lane % 16. All query rows and heads of a KV head share the rows.
 //   O^T = V^T P^T  A = V^T: lane % 16 stands for the CP columns whose piece of a row the lane has loaded, and one product per
-//                  column of a piece takes that column of its tokens 4 (lane / 16) + j: in bf16 byte permutes inside the
-//                  lane, no transposition. B = P^T is what the first product left in the lane. O^T and the running maximum have the pair in
-//                  lane % 16 both, so a rescale needs no exchange either.
+//                  column of a piece takes that column of its tokens 4 (lane / 16) + j: in bf16 byte permutes inside the lane,
+//                  no transposition. B = P^T is what the first product left in the lane. O^T and the running maximum both have
+//                  the pair in lane % 16, so a rescale needs no exchange either.
 // bf16 probabilities enter as p = hi + lo, two bf16 parts (the matrix cores are idle otherwise): the result is off by its own
 // rounding only. fp32 runs the fp32 matrix cores.
-// The tiles of all sequences, KV heads and blocks of 16 pairs lie in one row, of which every workgroup takes an even share, whatever
-// the lengths (paged_walk.h); its four wavefronts take every fourth tile and merge in LDS. Where a problem's tiles lie in several shares,
-// the workgroup that finishes last (a ticket) adds the partial results up in order, so results do not depend on who that was.
+// The tiles of all sequences, KV heads and blocks of pairs lie in one row, of which every workgroup takes an even share, whatever
+// the lengths (paged_walk.h); its wavefronts take its tiles in turn and merge in LDS. Where a problem's tiles lie in several shares,
+// the workgroup that finishes last (a ticket), or a launch of its own, adds the partial results up in order, so results do not
+// depend on who that was. Two workgroups a compute unit: with three the tile loop spills (1839 us for the first case above). The
+// last tenth of the row in short shares for whoever is done first (dies end 5 to 10 % apart): what a share costs to begin is more.
 #include <algorithm>
 
 #include "device_common.h"
@@ -69,14 +74,16 @@ __device__ __forceinline__ float max_quarters(float v) {
 }
 __device__ __forceinline__ bool not_finite_f32(uint32_t x) { return (x & 0x7f800000u) == 0x7f800000u; }
 __device__ __forceinline__ bool not_finite_bf16x2(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
-__device__ __forceinline__ unsigned long long two_floats(float x, float y) { return ((unsigned long long)__float_as_uint(y) << 32) | __float_as_uint(x); }
+__device__ __forceinline__ unsigned long long two_floats(float x, float y) {
+  return ((unsigned long long)__float_as_uint(y) << 32) | __float_as_uint(x);
+}
 __device__ __forceinline__ float first_float(unsigned long long v) { return __uint_as_float((uint32_t)v); }
 __device__ __forceinline__ float second_float(unsigned long long v) { return __uint_as_float((uint32_t)(v >> 32)); }
 __device__ __forceinline__ float safe_ref(float m) { return m == -INFINITY ? 0.f : m; }
 
 // A wavefront's matrix products of one tile, by type. NU: groups of 16 tokens in a tile; VW: 32-bit words of a lane's piece of a value row.
-// ONCE: no other wavefront reads these rows: they pass the caches by. 16 x 128K tokens 1394 -> 1268 us, 64 ragged sequences 193 -> 180; where wavefronts share
-// rows (16 query rows over 32K) it is 59 -> 85.
+// ONCE: no other wavefront reads these rows: they pass the caches by. 16 x 128K tokens 1394 -> 1268 us, 64 ragged sequences
+// 193 -> 180; where wavefronts share rows (16 query rows over 32K) it is 59 -> 85.
 template <bool ONCE, class T> __device__ __forceinline__ T load_row(const char* p) {
   if constexpr (ONCE) return __builtin_nontemporal_load((const T*)p);
   else return *(const T*)p;
@@ -102,8 +109,13 @@ template <int DIM, bool ONCE> struct TileOps<LTRI_BF16, DIM, ONCE> {
     for (int i = 0; i < NK; ++i) *(u32x4_t*)(row + i * 64 + g * 16) = k[u][i];
   }
   __device__ __forceinline__ void load_v(int u, int j, const char* row, int kl) {    // row: of token 16 u + 4 (lane / 16) + j
-    if constexpr (VW == 4) { const u32x4_t x = load_row<ONCE, u32x4_t>(row + kl * 16); v[u][j][0] = x[0]; v[u][j][1] = x[1]; v[u][j][2] = x[2]; v[u][j][3] = x[3]; }
-    else { const u32x2_t x = load_row<ONCE, u32x2_t>(row + kl * 8); v[u][j][0] = x[0]; v[u][j][1] = x[1]; }
+    if constexpr (VW == 4) {
+      const u32x4_t x = load_row<ONCE, u32x4_t>(row + kl * 16);
+      v[u][j][0] = x[0]; v[u][j][1] = x[1]; v[u][j][2] = x[2]; v[u][j][3] = x[3];
+    } else {
+      const u32x2_t x = load_row<ONCE, u32x2_t>(row + kl * 8);
+      v[u][j][0] = x[0]; v[u][j][1] = x[1];
+    }
   }
   __device__ __forceinline__ void store_v(int u, int j, char* row, int kl) const {
     if constexpr (VW == 4) *(u32x4_t*)(row + kl * 16) = u32x4_t{v[u][j][0], v[u][j][1], v[u][j][2], v[u][j][3]};
@@ -128,7 +140,7 @@ template <int DIM, bool ONCE> struct TileOps<LTRI_BF16, DIM, ONCE> {
         s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[u][i]), __builtin_bit_cast(bf16x8_t, q[i]), s[u], 0, 0, 0);
     }
   }
-  // o += V^T P^T. APART: only the lane's tokens [u][j] whose bit 4 u + j of vis is set count, and only the pairs of lanes with `mine` take the sum.
+  // o += V^T P^T. APART: only the lane's tokens [u][j] whose bit 4 u + j of vis is set count, and only lanes with `mine` take the sum.
   template <bool APART>
   __device__ __forceinline__ void values(const f32x4_t (&p)[NU], uint32_t vis, bool mine) {
     u32x4_t hi, lo;
@@ -280,8 +292,9 @@ __device__ __forceinline__ void write_result(const PagedCall& a, size_t r, int c
   }
 }
 
-// WB blocks of 16 pairs to a problem: a wavefront has block wave % WB, and every (PA_WAVES / WB)-th tile of the share. The blocks' wavefronts go through
-// the same tiles side by side, so that one reads from memory what the others find in the compute unit's cache.
+// WB blocks of 16 pairs to a problem: a wavefront has block wave % WB, and every (PA_WAVES / WB)-th tile of the share. The blocks'
+// wavefronts go through the same tiles side by side, so that one reads from memory what the others find in the compute unit's
+// cache (two or four blocks to a wavefront need more registers than there are: 16 rows of 4 heads over 32K tokens 80 us, this 55).
 // SMALL: pages of fewer than 16 tokens, whose page is looked up lane by lane; else a group of 16 tokens lies in one page.
 template <int DT, int DIM, int WB, bool SMALL>
 __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCall a, int min_share, int merge_later) {
@@ -359,9 +372,9 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
     for (int t = 0; t < NT; ++t) ops.o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
 
-    // Pages of a tile: of its groups of 16 tokens, by scalar loads (the table does not change while a launch runs), or (SMALL) of the token that
-    // the lane loads of every group's keys and of its four of the values. Past the sequence's end the last token's. They are asked for before the
-    // rows of the tile in front, so that the loads, which come back in order, need not be waited for to have them.
+    // Pages of a tile: of its groups of 16 tokens, by scalar loads (the table does not change while a launch runs), or (SMALL) of the
+    // token that the lane loads of every group's keys and of its four of the values. Past the sequence's end the last token's. They
+    // are asked for before the rows of the tile in front, so that the loads, which come back in order, need not be waited for.
     struct Pages { int k[NU], v[NU][SMALL ? 4 : 1]; };
     auto look_up = [&](int t, Pages& p) __attribute__((always_inline)) {
 #pragma unroll
@@ -661,7 +674,7 @@ __global__ __launch_bounds__(WALK_T) void paged_merge_kernel(PagedCall a, int wg
   if (parts == 1) return;
   __shared__ __align__(16) float s_o[WALK_T / 64][2][DIM];
   __shared__ float s_m[WALK_T / 64][2], s_l[WALK_T / 64][2];
-  constexpr int LANES = DIM / 4, SIDES = 64 / LANES < 2 ? 1 : 2;               // the lanes of a wavefront that take other parts of the same columns
+  constexpr int LANES = DIM / 4, SIDES = 2;      // lanes of a row; so many of them side by side take other parts
   const int side = lane / LANES, c = lane % LANES * 4;
   if (side < SIDES) {
     f32x4_t o;
@@ -687,7 +700,7 @@ __global__ __launch_bounds__(WALK_T) void paged_merge_kernel(PagedCall a, int wg
 }
 
 // Weights from the scores: w <- decay w + sum over the KV head's pairs of exp(s - lse). A wavefront takes 256 tokens of a KV head at a
-// time, a lane four of them; the pieces are shared out like the tiles above.
+// time, a lane four of them; the pieces are shared out like the tiles above. 16 x 16K tokens of 32 heads: 16 us for 50 MB.
 constexpr int PW_TOKENS = 256;
 template <int TILE>
 __global__ __launch_bounds__(WALK_T) void paged_weights_kernel(PagedCall a) {
@@ -750,15 +763,17 @@ __global__ __launch_bounds__(WALK_T) void paged_weights_kernel(PagedCall a) {
   }
 }
 
-// The same from the keys, for many pairs (see paged_keeps_scores): the scores again, one tile of keys after the other, with the log-sum-exps at hand.
-// The queries of 64 pairs stay in registers; the next tile's keys are on their way while one is used.
+// The same from the keys, for many pairs (see paged_keeps_scores): the scores again, one tile of keys after the other, with the
+// log-sum-exps at hand. The queries of 64 pairs stay in registers; the next tile's keys are on their way while one is used.
+// 64 pairs over 32K tokens, 8 KV heads: 18 us for 67 MB of keys.
 template <int DT, int DIM>
 __global__ __launch_bounds__(WALK_T, 2) void paged_key_weights_kernel(PagedCall a) {
   constexpr int T = PagedTile<DT>::N, ELT = DT == LTRI_F32 ? 4 : 2, WAVES = WALK_T / 64, NB = 4;
   typedef TileOps<DT, DIM, true> Ops;
   constexpr int NU = Ops::NU;
   const PagedDims& D = a.D;
-  const int pairs = a.n * D.G, w = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kl = lane & 15, g = lane >> 4;
+  const int pairs = a.n * D.G, w = blockIdx.x, lane = threadIdx.x & 63, kl = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float sc = LOG2E / sqrtf((float)DIM);
   const int tok_bytes = (int)D.token_stride * ELT;
   long long share = 0;
@@ -827,7 +842,8 @@ __global__ __launch_bounds__(WALK_T, 2) void paged_key_weights_kernel(PagedCall 
         Pages after;
         look_up(min(t + 2 * WAVES, nt - 1), after);
         if (t + WAVES < t1) load_k(t + WAVES, next);
-        // a lane's sums of its tokens 16 u + 4 g + j over the blocks, then over the 16 lanes that hold a token's pairs; lane 4 u + j keeps token 4 g + j of group u
+        // a lane's sums of its tokens 16 u + 4 g + j over the blocks, then over the 16 lanes that hold a token's pairs; lane 4 u + j
+        // keeps token 4 g + j of group u
         float sum = 0.f;
 #pragma unroll
         for (int u = 0; u < NU; ++u)
@@ -882,8 +898,9 @@ static void launch_key_weights(const PagedCall& a, int wgs, hipStream_t s) {
   else paged_key_weights_kernel<DT, 128><<<wgs, WALK_T, 0, s>>>(a);
 }
 
-// A launch of its own for the merge from this many bytes of a problem's partial results on. One sequence, 8 KV heads of 4: 128K tokens (131 KB) 107.5 us
-// with the last workgroup, 104.9 with the launch; 32K tokens of 16 rows (2 MB) 147 and 60; fp32, 2 x 4097 tokens of one KV head, 64 wide (66 KB) 12.7 and 15.3.
+// A launch of its own for the merge from this many bytes of a problem's partial results on. One sequence, 8 KV heads of 4: 128K
+// tokens (131 KB) 107.5 us with the last workgroup, 104.9 with the launch; 32K tokens of 16 rows (2 MB) 147 and 60; fp32, 2 x 4097
+// tokens of one KV head, 64 wide (66 KB) 12.7 and 15.3.
 constexpr long long MERGE_BYTES = 96 << 10;
 
 hipError_t launch_paged_attend(const PagedCall& a, hipStream_t s) {

@@ -8,17 +8,19 @@
 namespace ltri {
 
 constexpr int PAGED_TILE = 32;             // rows of scores are padded to at most this many tokens
-// Tiles that the beginning and end of a (sequence, KV head, block of pairs) are as long as. 256 sequences of up to 2000 tokens, us: 2: 144, 4: 121,
-// 8: 114, 14: 121; 64 of up to 4096: 72, 67, 67, 68; even batches do not depend on it.
+// Tiles that the beginning and end of a (sequence, KV head, block of pairs) are as long as. 256 sequences of up to 2000 tokens, us:
+// 2: 144, 4: 121, 8: 114, 14: 121; 64 of up to 4096: 72, 67, 67, 68; even batches do not depend on it.
 constexpr int PAGED_EXTRA = 8;
 constexpr int PAGED_MAX_WGS = 1024;        // workgroups of an attention launch, at most
-// Whether an attention with weights leaves its scores in scratch for them (8 bytes a token and pair, written and read), or the keys are read
-// again (2 to 4 head_dim bytes a token): from 32 pairs on that is less, and the scratch need not hold scores of many rows.
-// 16 rows of 4 heads over 32K tokens, 8 KV heads: scores 54 us (20 of it their writes), keys 24; 4 rows: scores 16; 8 rows (32 pairs): keys 20.
+// Whether an attention with weights leaves its scores in scratch for them (8 bytes a token and pair, written and read), or the keys
+// are read again (2 to 4 head_dim bytes a token): from 32 pairs on that is less, and the scratch need not hold scores of many rows.
+// 16 rows of 4 heads over 32K tokens, 8 KV heads: scores 54 us (20 of it their writes), keys 18; 8 rows: keys 15; 4 rows: scores 16.
 constexpr int PAGED_SCORE_PAIRS = 31;
 __host__ __device__ constexpr bool paged_keeps_scores(int pairs) { return pairs <= PAGED_SCORE_PAIRS; }
 
-// Eviction: tables of up to EV_LONG tokens are selected from by one workgroup per (sequence, KV head), longer ones by several.
+// Eviction: tables of up to EV_LONG tokens are selected from by one workgroup per (sequence, KV head), longer ones by several, EV_CHUNK
+// tokens each. One sequence of 8 KV heads, us with its append of 2K to 4K: one workgroup 16K tokens 42, 22K 52, 32K 60; several 17K
+// tokens 49, 34K 49.
 constexpr int EV_LONG = 16384, EV_CHUNK = 8192;
 constexpr int EV_LONG_WORDS = 4 + 2048;    // counters of a (sequence, KV head), zero between launches
 constexpr int EV_SLOT_BYTES = 24;          // what the launches of a long selection tell each other
