@@ -242,8 +242,9 @@ template <int DIM, bool ONCE> struct TileOps<LTRI_F32, DIM, ONCE> {
   }
 };
 
-// Sum of a problem's partial results of four columns of a pair: the parts first, first + step, ..., eight in flight. block: pairs of a problem.
-template <int DIM>
+// Sum of a problem's partial results of four columns of a pair: the parts first, first + step, ..., eight in flight. block: pairs of a
+// problem. SAME: written by the same launch (device scope, see wait_for_own_stores).
+template <int DIM, bool SAME>
 __device__ __forceinline__ void add_parts(const PagedCall& a, int block, int w0, int parts, int first, int step, int p, int c, f32x4_t& o, float& top,
                                           float& sum) {
   constexpr int DEEP = 8;
@@ -251,15 +252,23 @@ __device__ __forceinline__ void add_parts(const PagedCall& a, int block, int w0,
   sum = 0.f;
   o = f32x4_t{0.f, 0.f, 0.f, 0.f};
   for (int k0 = first; k0 < parts; k0 += step * DEEP) {
-    unsigned long long ml[DEEP], lo[DEEP], hi[DEEP];
+    unsigned long long ml[DEEP];
+    f32x4_t part[DEEP];
 #pragma unroll
     for (int u = 0; u < DEEP; ++u) {
       const int k = min(k0 + step * u, parts - 1);
       const size_t at_part = (2 * (size_t)(w0 + k) + (k == 0)) * block + p;
-      const unsigned long long* from = (const unsigned long long*)(a.part + at_part * DIM + c);
-      ml[u] = __hip_atomic_load(a.part_ml + at_part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      lo[u] = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      hi[u] = __hip_atomic_load(from + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const float* from = a.part + at_part * DIM + c;
+      if constexpr (SAME) {
+        const unsigned long long* two = (const unsigned long long*)from;
+        ml[u] = __hip_atomic_load(a.part_ml + at_part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const unsigned long long lo = __hip_atomic_load(two, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const unsigned long long hi = __hip_atomic_load(two + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        part[u] = f32x4_t{first_float(lo), second_float(lo), first_float(hi), second_float(hi)};
+      } else {
+        ml[u] = a.part_ml[at_part];
+        part[u] = *(const f32x4_t*)from;
+      }
     }
     float most = top;
 #pragma unroll
@@ -273,7 +282,7 @@ __device__ __forceinline__ void add_parts(const PagedCall& a, int block, int w0,
       if (k0 + step * u >= parts) continue;
       const float e = __builtin_amdgcn_exp2f(first_float(ml[u]) - ref);
       sum = fmaf(e, second_float(ml[u]), sum);
-      o += e * f32x4_t{first_float(lo[u]), second_float(lo[u]), first_float(hi[u]), second_float(hi[u])};
+      o += e * part[u];
     }
   }
 }
@@ -617,6 +626,13 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
       join(result);
       continue;
     }
+    if (merge_later) {
+      join([&](int p, int c, f32x4_t o, float top, float sum) __attribute__((always_inline)) {
+        *(f32x4_t*)(a.part + (slot * PB + p) * DIM + c) = o;
+        if (c == 0) a.part_ml[slot * PB + p] = two_floats(top, sum);
+      });
+      continue;
+    }
     join([&](int p, int c, f32x4_t o, float top, float sum) __attribute__((always_inline)) {       // device scope (see wait_for_own_stores)
       unsigned long long* to = (unsigned long long*)(a.part + (slot * PB + p) * DIM + c);
       __hip_atomic_store(to, two_floats(o[0], o[1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -624,7 +640,6 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
       if (c == 0) __hip_atomic_store(a.part_ml + slot * PB + p, two_floats(top, sum), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     });
     const int w0 = (int)(problem / share), parts = (int)((problem + nt - 1) / share) - w0 + 1;      // the workgroups that share the problem
-    if (merge_later) continue;
     wait_for_own_stores();
     __syncthreads();
     int32_t* ticket = a.tickets + ((size_t)s * D.Hkv + h) * blocks + pb;
@@ -637,7 +652,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
         const int p = i / (DIM / 4), c = i % (DIM / 4) * 4;
         f32x4_t o;
         float top, sum;
-        add_parts<DIM>(a, PB, w0, parts, wave, PA_WAVES, p, c, o, top, sum);
+        add_parts<DIM, true>(a, PB, w0, parts, wave, PA_WAVES, p, c, o, top, sum);
         *(f32x4_t*)&s_o[wave][p][c] = o;
         if (c == 0) { s_m[wave][p] = top; s_l[wave][p] = sum; }
       }
@@ -648,7 +663,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
         const int p = i / (DIM / 4), c = i % (DIM / 4) * 4;
         f32x4_t o;
         float top, sum;
-        add_parts<DIM>(a, PB, w0, parts, 0, 1, p, c, o, top, sum);
+        add_parts<DIM, true>(a, PB, w0, parts, 0, 1, p, c, o, top, sum);
         result(p, c, o, top, sum);
       }
     }
@@ -679,7 +694,7 @@ __global__ __launch_bounds__(WALK_T) void paged_merge_kernel(PagedCall a, int wg
   if (side < SIDES) {
     f32x4_t o;
     float top, sum;
-    add_parts<DIM>(a, block, w0, parts, wave * SIDES + side, WALK_T / 64 * SIDES, pair % block, c, o, top, sum);
+    add_parts<DIM, false>(a, block, w0, parts, wave * SIDES + side, WALK_T / 64 * SIDES, pair % block, c, o, top, sum);
     *(f32x4_t*)&s_o[wave][side][c] = o;
     if (c == 0) { s_m[wave][side] = top; s_l[wave][side] = sum; }
   }
