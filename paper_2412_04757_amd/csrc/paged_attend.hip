@@ -434,10 +434,11 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
     };
 
     Pages now, next;
-    // One tile; EDGE: see `edge`.
-    auto tile = [&](int t, auto edge_c) __attribute__((always_inline)) {
-      constexpr bool EDGE = decltype(edge_c)::value, AHEAD = SMALL || !EDGE;
-      if constexpr (!AHEAD) {
+    // One tile; EDGE: see `edge`; MORE: the wavefront's next tile follows, and its rows are asked for. (With a condition in the loop in
+    // its place the compiler, which then cannot count the loads on their way, waits for the values before the keys are used.)
+    auto tile = [&](int t, auto edge_c, auto more_c) __attribute__((always_inline)) {
+      constexpr bool EDGE = decltype(edge_c)::value, MORE = decltype(more_c)::value;
+      if constexpr (EDGE && !SMALL) {
         look_up(t, now);
         load_k(t, now, edge_c);
         load_v(t, now, edge_c);
@@ -460,11 +461,10 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
           }
         }
       }
-      const bool more = AHEAD && t + STEP < (SMALL ? t1 : edge);
       Pages after;
-      if constexpr (AHEAD) {
+      if constexpr (MORE) {
         look_up(min(t + 2 * STEP, nt - 1), after);
-        if (more) load_k(t + STEP, next, edge_c);
+        load_k(t + STEP, next, edge_c);
         __builtin_amdgcn_sched_barrier(0);
       }
 
@@ -559,9 +559,9 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
         }
       }
       if (!apart) ops.template values<false>(sv, 0u, true);
-      if constexpr (AHEAD) {
+      if constexpr (MORE) {
         __builtin_amdgcn_sched_barrier(0);
-        if (more) load_v(t + STEP, next, edge_c);
+        load_v(t + STEP, next, edge_c);
         __builtin_amdgcn_sched_barrier(0);
         now = next;
         next = after;
@@ -569,18 +569,21 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
     };
     int t = t0 + wave / WB;
     if (pair0 >= pairs) t = t1;                                      // a block without pairs
-    if (t < (SMALL ? t1 : edge)) {
-      constexpr std::integral_constant<bool, SMALL> small_c{};
+    constexpr std::integral_constant<bool, SMALL> small_c{};
+    const int end = SMALL ? t1 : edge;
+    if (t < end) {
       look_up(t, now);
       look_up(min(t + STEP, nt - 1), next);
       load_k(t, now, small_c);
       __builtin_amdgcn_sched_barrier(0);                             // keys before values, as in the loop: what is waited for first comes first
       load_v(t, now, small_c);
       __builtin_amdgcn_sched_barrier(0);
+      for (; t + STEP < end; t += STEP) tile(t, small_c, std::true_type{});
+      tile(t, small_c, std::false_type{});
+      t += STEP;
     }
     if constexpr (!SMALL)
-      for (; t < edge; t += STEP) tile(t, std::false_type{});
-    for (; t < t1; t += STEP) tile(t, std::true_type{});
+      for (; t < t1; t += STEP) tile(t, std::true_type{}, std::false_type{});
 
     // the wavefronts' results: own maximum, sum and O
     l = over_quarters(l);
