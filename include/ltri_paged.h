@@ -83,7 +83,7 @@ int32_t ltri_paged_set_stream(ltri_paged* c, void* hip_stream);
 int32_t ltri_paged_append(ltri_paged* c, int32_t seq_count, const int32_t* table, const int32_t* lens,
                           const int32_t* seen, const void* k_new, const void* v_new, const float* w_new, int32_t n_new);
 
-/* q: device [seq_count][n_q][n_q_heads][head_dim], out the same, in the dtype; lse: device fp32
+/* q: device [seq_count][n_q][n_q_heads][head_dim], out the same, in the dtype, not overlapping; lse: device fp32
  * [seq_count][n_q][n_q_heads] or NULL (natural-log sum of exponentials of the scaled scores). Row i attends the tokens
  * 0 .. lens - n_q + i, with weights softmax(q.k / sqrt(head_dim)); a row that sees no token, or whose scores are all
  * -infinity, gives 0 and -infinity. Rows of tokens it does not see have no influence, whatever they hold; an infinity or NaN in

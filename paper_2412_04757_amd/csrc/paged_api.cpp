@@ -60,6 +60,7 @@ static int32_t derive(const ltri_paged_config* cfg, PagedDims& D, PagedLayout& L
     for (const Axis& x : ax) {
       if (x.count == 1) *x.stride = 0;                  // never stepped over, whatever was given
       else if (*x.stride < 1 || *x.stride % step || *x.stride > 1ll << 40) return LTRI_EINVAL;
+      if ((double)x.count * *x.stride * D.elt > 4e18) return LTRI_EINVAL;      // (sums of three stay within 63 bits)
     }
     if (D.token_stride > 1ll << 24) return LTRI_EINVAL;     // 16 tokens lie within 32-bit byte offsets
     // no two rows may overlap: in the order of the strides, each steps over all that the axes below it reach
@@ -223,10 +224,12 @@ static int32_t check_rows(ltri_paged* c, const void* k_new, const void* v_new) {
   return LTRI_OK;
 }
 
-static int32_t check_query(ltri_paged* c, const void* q, int32_t n_q, void* out, float* lse, float decay) {
+static int32_t check_query(ltri_paged* c, int32_t seq_count, const void* q, int32_t n_q, void* out, float* lse, float decay) {
   if (n_q < 1 || n_q > c->D.rows_max) return fail(c, LTRI_EINVAL, "%d query rows outside [1, rows_max %d]", n_q, c->D.rows_max);
   if (!q || !out) return fail(c, LTRI_EINVAL, "q or out is NULL");
   if (misaligned(q, 16) || misaligned(out, 16) || misaligned(lse, 4)) return fail(c, LTRI_EINVAL, "q and out must be 16-byte aligned, lse 4-byte");
+  const uintptr_t bytes = (uintptr_t)seq_count * n_q * c->D.Hq * c->D.d * c->D.elt, from = (uintptr_t)q, to = (uintptr_t)out;
+  if (from < to + bytes && to < from + bytes) return fail(c, LTRI_EINVAL, "q and out overlap");      // (weights read q again)
   if (!(std::fabs(decay) <= 3.4028234e38f)) return fail(c, LTRI_EINVAL, "decay is not a finite number");
   if (decay >= 0.0f && !c->D.weights) return fail(c, LTRI_EINVAL, "decay %g, but the cache keeps no weights", (double)decay);
   return LTRI_OK;
@@ -256,7 +259,7 @@ int32_t ltri_paged_attend(ltri_paged* c, int32_t seq_count, const int32_t* table
   if (!c) return LTRI_EINVAL;
   PagedCall a;
   int32_t r = begin(c, seq_count, table, lens, nullptr, false, a);
-  if (r == LTRI_OK) r = check_query(c, q, n_q, out, lse, decay);
+  if (r == LTRI_OK) r = check_query(c, seq_count, q, n_q, out, lse, decay);
   if (r != LTRI_OK) return r;
   a.q = q; a.n = n_q; a.out = out; a.lse = lse; a.decay = decay;
   if (c->dry) return LTRI_OK;
@@ -270,7 +273,7 @@ int32_t ltri_paged_step(ltri_paged* c, int32_t seq_count, const int32_t* table, 
   if (!c) return LTRI_EINVAL;
   PagedCall a;
   int32_t r = begin(c, seq_count, table, lens, seen, c->D.weights != 0, a);
-  if (r == LTRI_OK) r = check_query(c, q, n_new, out, lse, decay);
+  if (r == LTRI_OK) r = check_query(c, seq_count, q, n_new, out, lse, decay);
   if (r == LTRI_OK) r = check_rows(c, k_new, v_new);
   if (r != LTRI_OK) return r;
   a.k_new = k_new; a.v_new = v_new; a.q = q; a.n = n_new; a.out = out; a.lse = lse; a.decay = decay;

@@ -58,7 +58,10 @@ class LtriPagedCache:
             return
         self.device = device = torch.device(device.type, torch.cuda.current_device() if device.index is None else device.index)
         self._index = device.index
-        with torch.cuda.device(device):
+        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+        if self.stream.device != device:
+            raise ValueError(f"a stream of {self.stream.device}, the cache is on {device}")
+        with torch.cuda.stream(self.stream):                 # (what is allocated here is filled and used there)
             if k_pages is None:
                 k_pages = torch.zeros(shape, dtype=self.tdtype, device=device)
                 v_pages = torch.zeros(shape, dtype=self.tdtype, device=device)
@@ -78,7 +81,6 @@ class LtriPagedCache:
             self.k_pages, self.v_pages, self.weight, self.pos = k_pages, v_pages, weight, pos
             self.state = torch.empty(self.state_bytes, dtype=torch.uint8, device=device)
             self.scratch = torch.empty(self.scratch_bytes, dtype=torch.uint8, device=device) if scratch is None else scratch
-            self.stream = stream if stream is not None else torch.cuda.current_stream(device)
             self._check(self.lib.ltri_paged_create(C.byref(cfg), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(weight), _ptr(pos),
                                                    self.state.data_ptr(), _ptr(self.scratch), self.stream.cuda_stream,
                                                    C.byref(self.handle)))
@@ -114,20 +116,26 @@ class LtriPagedCache:
                 self._arg("seen", seen, (n,), torch.int32))
 
     def _rows(self, n: int, k_new: torch.Tensor, v_new: torch.Tensor):
-        c, n_new = self.cfg, k_new.shape[2]
+        c, n_new = self.cfg, k_new.shape[2] if k_new.dim() == 4 else 0
         shape = (n, c.n_kv_heads, n_new, c.head_dim)
         return self._arg("k_new", k_new, shape, self.tdtype), self._arg("v_new", v_new, shape, self.tdtype), n_new
 
     def _outputs(self, n: int, q: torch.Tensor, out, lse):
-        c, n_q = self.cfg, q.shape[1]
+        c, n_q = self.cfg, q.shape[1] if q.dim() == 4 else 0
         shape = (n, n_q, c.n_q_heads, c.head_dim)
         q_ptr = self._arg("q", q, shape, self.tdtype)
         if out is None:
-            out = torch.empty_like(q)
+            if self.dry or torch.cuda.current_stream(self._index) == self.stream:
+                out = torch.empty_like(q)
+            else:                                            # its memory belongs to the stream that writes it
+                with torch.cuda.stream(self.stream):
+                    out = torch.empty_like(q)
         return q_ptr, n_q, out, self._arg("out", out, shape, self.tdtype), self._arg("lse", lse, shape[:3], torch.float32)
 
     # ---- the C ABI, same names ----
     def set_stream(self, stream: "torch.cuda.Stream") -> None:
+        if not self.dry and stream.device != self.device:
+            raise ValueError(f"a stream of {stream.device}, the cache is on {self.device}")
         self._check(self.lib.ltri_paged_set_stream(self.handle, stream.cuda_stream))
         self.stream = stream
 
@@ -153,8 +161,8 @@ class LtriPagedCache:
         """ltri_paged_step: append (weights of new tokens 0) and attend of the same rows."""
         n, t, l, s = self._places(table, lens, seen)
         k, v, n_new = self._rows(n, k_new, v_new)
-        if q.shape[1] != n_new:
-            raise ValueError(f"{q.shape[1]} query rows for {n_new} new tokens")
+        if q.shape[1:2] != (n_new,):
+            raise ValueError(f"q {tuple(q.shape)} for {n_new} new tokens")
         q_ptr, _, out, o_ptr, lse_ptr = self._outputs(n, q, out, lse)
         self._check(self.lib.ltri_paged_step(self.handle, n, t, l, s, k, v, q_ptr, n_new, o_ptr, lse_ptr,
                                              -1.0 if decay is None else decay))

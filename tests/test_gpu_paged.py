@@ -135,8 +135,8 @@ def test_a_row_is_not_touched_by_tokens_it_does_not_see(gpu_device, dtype):
     with np.errstate(invalid="ignore"):
         want, want_lse = c.oracle_attend()
     t = c.tolerances()
-    assert (np.abs(out - want)[:, :2] <= t["out_abs"] + 1.01 * t["out_rel"] * np.abs(want[:, :2])).all()
-    assert (np.abs(lse.cpu().numpy() - want_lse)[:, :2] <= t["lse"]).all()
+    assert (np.abs(out[:, :2] - want[:, :2]) <= t["out_abs"] + 1.01 * t["out_rel"] * np.abs(want[:, :2])).all()
+    assert (np.abs(lse.cpu().numpy()[:, :2] - want_lse[:, :2]) <= t["lse"]).all()
     assert not np.isfinite(out[:, 2, :4, ::3]).any() and np.isnan(out[:, 2, 4:]).all()
 
 
@@ -158,7 +158,7 @@ def test_scores_of_any_size(gpu_device, dtype):
     # a score of 3e4 / sqrt(128), in the log2 domain, is held to 2^-24 of 3.9e3: its probability to 2^-12
     vmax = np.nanmax(np.abs(c.v))
     assert (np.abs(got - want) <= 2.0 ** -10 * vmax + 1.01 * torch.finfo(TYPES[dtype]).eps / 2 * np.abs(want)).all()
-    assert (np.abs(got_lse - want_lse)[:3] <= 2.0 ** -10).all()
+    assert (np.abs(got_lse[:3] - want_lse[:3]) <= 2.0 ** -10).all()
     assert (got[3] == 0).all() and np.isneginf(got_lse[3]).all()
 
 
@@ -480,6 +480,30 @@ def test_work_goes_to_the_stream_that_is_set(gpu_device):
     c.cache.attend(*c.args(False), q, out=out)
     side.synchronize()
     c.check_attend(out, None, *c.oracle_attend())
+
+
+def test_a_cache_of_another_stream_than_the_current_one(gpu_device):
+    """What it allocates (pools, results) is filled on its own stream, whatever the current one is busy with."""
+    c = Case(gpu_device, [900, 20], weights=False)
+    k, v = np.zeros((2, c.hkv, 900, c.dim)), np.zeros((2, c.hkv, 900, c.dim))
+    for s, n in enumerate(c.lens):
+        i = np.arange(n)
+        for to, pool in ((k, c.k), (v, c.v)):
+            to[s, :, 900 - n:] = pool[c.table[s][i // c.page], :, i % c.page].transpose(1, 0, 2)
+    rows = c.on(k), c.on(v)
+    args, q, busy = c.args(False), c.on(c.q), torch.randn((4096, 4096), device=gpu_device)
+    side = torch.cuda.Stream(gpu_device)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        busy = busy @ busy
+    cache = LtriPagedCache(c.cache.cfg, gpu_device, stream=side)
+    cache.append(*args, None, *rows)
+    out = cache.attend(*args, q)
+    for _ in range(4):                                    # (results take memory of that stream: nothing of the current one lands in them)
+        torch.empty_like(q).fill_(7.0)
+    torch.cuda.synchronize()
+    c.check_attend(out, None, *c.oracle_attend())
+    assert cache.sync_status() == 0
 
 
 def test_two_caches_share_a_scratch(gpu_device):

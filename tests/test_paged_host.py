@@ -32,6 +32,7 @@ def sizes(cfg):
     dict(page_stride=2048, head_stride=512, token_stride=64),             # heads overlap
     dict(page_stride=1024, head_stride=1024, token_stride=64),            # pages overlap
     dict(page_stride=-2048, head_stride=1024, token_stride=64),
+    dict(n_pages=2147483647, page_stride=1 << 39, head_stride=1 << 40, token_stride=64),      # beyond 63 bits
 ])
 def test_unsupported_configurations_are_refused(kw):
     assert sizes(config(**kw))[0] == EINVAL
@@ -81,7 +82,7 @@ class Address:
 def call(cache, name, **kw):
     """A call with good arguments but those given."""
     lib, h = cache.lib, cache.handle
-    a = dict(n=2, table=256, lens=256, seen=256, k=256, v=256, w=256, rows=1, q=256, out=256, lse=256, decay=1.0, keep=20, sink=4, recent=8)
+    a = dict(n=2, table=256, lens=256, seen=256, k=256, v=256, w=256, rows=1, q=256, out=65536, lse=256, decay=1.0, keep=20, sink=4, recent=8)
     a.update(kw)
     if name == "append":
         return lib.ltri_paged_append(h, a["n"], a["table"], a["lens"], a["seen"], a["k"], a["v"], a["w"], a["rows"])
@@ -106,6 +107,8 @@ EVERY = ("append", "attend", "step", "evict")
     (("attend", "step"), dict(q=260), EINVAL), (("attend", "step"), dict(out=264), EINVAL), (("attend", "step"), dict(lse=None), 0),
     (("attend", "step"), dict(lse=258), EINVAL), (("attend", "step"), dict(decay=float("nan")), EINVAL),
     (("attend", "step"), dict(decay=float("inf")), EINVAL), (("attend", "step"), dict(decay=-1.0), 0), (("attend", "step"), dict(decay=0.0), 0),
+    (("attend", "step"), dict(out=256), EINVAL), (("attend", "step"), dict(out=256 + 2048 - 16), EINVAL), (("attend", "step"), dict(out=256 + 2048), 0),
+    (("attend", "step"), dict(q=65536 + 2048 - 16), EINVAL), (("attend", "step"), dict(q=65536 + 2048), 0),      # 2 x 8 x 64 bf16: 2048 bytes
     (("evict",), dict(keep=0), EINVAL), (("evict",), dict(keep=-1), EINVAL), (("evict",), dict(sink=-1), EINVAL),
     (("evict",), dict(recent=-1), EINVAL), (("evict",), dict(keep=12), 0), (("evict",), dict(keep=11), EINVAL),
     (("evict",), dict(sink=2147483647, recent=2147483647), EINVAL), (("evict",), dict(keep=2147483647), 0),
@@ -139,12 +142,15 @@ def test_the_binding_checks_shapes_types_and_density():
            lambda: cache.append(t, n, n, k.transpose(1, 2), k), lambda: cache.append(t, n, n, k, k, w_new=torch.zeros(2, 2, 2)),
            lambda: cache.attend(t, n, q[:, :, :4]), lambda: cache.attend(t, n, q[:1]), lambda: cache.attend(t, n, q, lse=torch.zeros(2, 3)),
            lambda: cache.attend(t, n, q, out=q[:, :2]), lambda: cache.attend(t, n, q.float()), lambda: cache.step(t, n, n, k, k, q[:, :2].contiguous()),
+           lambda: cache.append(t, n, n, k[0], k[0]), lambda: cache.attend(t, n, q[0]), lambda: cache.step(t, n, n, k, k, q[0, 0, 0]),
            lambda: cache.attend(t, n, q.transpose(0, 1).contiguous().transpose(0, 1)), lambda: cache.evict(t, n[:1], n, 20)]
     for f in bad:
         with pytest.raises(ValueError):
             f()
     with pytest.raises(LtriError):
         cache.attend(t, n, torch.zeros((2, 5, 8, 64), dtype=torch.bfloat16))
+    with pytest.raises(LtriError):
+        cache.attend(t, n, q, out=q)
     with pytest.raises(ValueError):
         paged_config(8, 2, 64, "fp16", 16, 12, 4, 3)
 
