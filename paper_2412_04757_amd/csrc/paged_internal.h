@@ -19,8 +19,8 @@ constexpr int PAGED_SCORE_PAIRS = 31;
 __host__ __device__ constexpr bool paged_keeps_scores(int pairs) { return pairs <= PAGED_SCORE_PAIRS; }
 
 // Eviction: tables of up to EV_LONG tokens are selected from by one workgroup per (sequence, KV head), longer ones by several, EV_CHUNK
-// tokens each. One sequence of 8 KV heads, us with its append of 2K to 4K: one workgroup 16K tokens 42, 22K 52, 32K 60; several 17K
-// tokens 49, 34K 49.
+// tokens each. One sequence of 8 KV heads, us with its append of 2K: one workgroup 16K tokens 43, 22K 52, 32K 60; several 22K tokens
+// 46, 32K 46.
 constexpr int EV_LONG = 16384, EV_CHUNK = 4096;
 constexpr int EV_LONG_WORDS = 4 + 2048;    // counters of a (sequence, KV head), zero between launches
 constexpr int EV_SLOT_BYTES = 24;          // what the launches of a long selection tell each other
