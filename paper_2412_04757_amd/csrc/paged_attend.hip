@@ -60,6 +60,16 @@ __device__ __forceinline__ int only_here(int x) {
   asm volatile("" : "+v"(x));
   return x;
 }
+// 16 bytes a lane from base + off into LDS at to + 16 lane, without registers; M0 needs a cycle before it is used.
+__device__ __forceinline__ void to_lds(const char* base, uint32_t off, uint32_t to) {
+  const uint64_t b = (uint64_t)(uintptr_t)base;
+  const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)b);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(all) : "m0", "memory");
+}
+// Until the wavefront has N loads under way at most and its reads of LDS are done, then for the other wavefronts.
+template <int N> __device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
   const bf16x2_t v = {(__bf16)lo, (__bf16)hi};
@@ -313,7 +323,12 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
   constexpr int PITCH = DIM + 4;
   static_assert(NU * 16 == T && WALK_T == 64 * PA_WAVES, "");
   constexpr int PB = 16 * WB, STEP = PA_WAVES / WB;                  // pairs of a problem, wavefronts of a block
-  __shared__ __align__(16) float s_o[PA_WAVES][16][PITCH];
+  // SHARED: tiles in LDS, 16 KB each, in the pieces that lanes take: STAGES in a ring; afterwards the wavefronts' O.
+  constexpr bool SHARED = WB == PA_WAVES && DIM == 128 && !SMALL;
+  constexpr int STAGES = 4, STAGE_BYTES = 16384, O_BYTES = sizeof(float) * PA_WAVES * 16 * PITCH;
+  static_assert(!SHARED || T * 2 * DIM * ELT == STAGE_BYTES, "");
+  __shared__ __align__(16) char s_mem[SHARED && STAGES * STAGE_BYTES > O_BYTES ? STAGES * STAGE_BYTES : O_BYTES];
+  float (*s_o)[16][PITCH] = (float (*)[16][PITCH])s_mem;
   __shared__ float s_m[PA_WAVES][16], s_l[PA_WAVES][16];
   __shared__ int s_last;
   const PagedDims& D = a.D;
@@ -366,7 +381,8 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
     const int all_see = len - a.n + 1 + min(pair0, pairs - 1) / D.G; // ... that every pair of the block sees
     // Tiles from here on: some token is not seen by some pair, or comes with the call. They take a way of their own, without the next
     // tile's rows on theirs; with SMALL pages every tile does, and has them.
-    const int edge = SMALL ? t0 : min(t1, max(0, min(all_see, first_new)) / T);
+    // (SHARED: the same for all wavefronts.)
+    const int edge = SMALL ? t0 : min(t1, max(0, min(SHARED ? len - a.n + 1 + pb * PB / D.G : all_see, first_new)) / T);
     const int32_t* table = a.table + (size_t)s * D.table_pages;
     const char* kh = a.k + (size_t)h * D.head_stride * ELT;
     const char* vh = a.v + (size_t)h * D.head_stride * ELT;
@@ -437,9 +453,12 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
     Pages now, next;
     // One tile; EDGE: see `edge`; MORE: the wavefront's next tile follows, and its rows are asked for. (With a condition in the loop in
     // its place the compiler, which then cannot count the loads on their way, waits for the values before the keys are used.)
-    auto tile = [&](int t, auto edge_c, auto more_c) __attribute__((always_inline)) {
+    auto tile = [&](int t, auto edge_c, auto more_c, const char* staged = nullptr) __attribute__((always_inline)) {
       constexpr bool EDGE = decltype(edge_c)::value, MORE = decltype(more_c)::value;
-      if constexpr (EDGE && !SMALL) {
+      if constexpr (SHARED && !EDGE) {
+#pragma unroll
+        for (int e = 0; e < NU * Ops::NK; ++e) ops.k[e / Ops::NK][e % Ops::NK] = *(const typename Ops::Piece*)(staged + e * 1024 + lane * 16);
+      } else if constexpr (EDGE && !SMALL) {
         look_up(t, now);
         load_k(t, now, edge_c);
         load_v(t, now, edge_c);
@@ -492,6 +511,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
 #pragma unroll
           for (int u = 0; u < NU; ++u)
             if (!good(now.k[u])) {
+              there &= ~(0xFu << (4 * u));
 #pragma unroll
               for (int j = 0; j < 4; ++j) ops.zero_v(u, j);
               sv[u] = f32x4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -507,7 +527,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
           if constexpr (EDGE) sv[u][j] = (vis >> (4 * u + j)) & 1 ? sv[u][j] : -INFINITY;
           mx = fmaxf(mx, sv[u][j]);
         }
-      if (scores && pair0 + kl < pairs) {
+      if (!SHARED && scores && pair0 + kl < pairs) {
 #pragma unroll
         for (int u = 0; u < NU; ++u) *(f32x4_t*)(scores + (size_t)t * T + 16 * u) = sv[u];
       }
@@ -526,6 +546,23 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
           sv[u][j] = __builtin_amdgcn_exp2f(sv[u][j] - ref);
           l += sv[u][j];
         }
+      if constexpr (SHARED && !EDGE) {
+        constexpr int PER = Ops::VW / 4;         // pieces of a lane's part of a value row
+#pragma unroll
+        for (int e = 0; e < NU * 4 * PER; ++e) {
+          const u32x4_t x = *(const u32x4_t*)(staged + STAGE_BYTES / 2 + e * 1024 + lane * 16);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ops.v[e / (4 * PER)][e / PER % 4][e % PER * 4 + i] = x[i];
+        }
+        if (there != 0xFFu) {                                        // (uniform)
+#pragma unroll
+          for (int u = 0; u < NU; ++u)
+            if (!((there >> (4 * u)) & 1)) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) ops.zero_v(u, j);
+            }
+        }
+      }
       bool apart = false;                        // an infinity or NaN in a token that some pair of the block does not see
       if constexpr (EDGE) {
         if (writes) {
@@ -572,7 +609,55 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCal
     if (pair0 >= pairs) t = t1;                                      // a block without pairs
     constexpr std::integral_constant<bool, SMALL> small_c{};
     const int end = SMALL ? t1 : edge;
-    if (t < end) {
+    if constexpr (SHARED) {
+      // Every wavefront brings a quarter of each tile, STAGES - 1 tiles ahead, in a row of pages it looks up one tile sooner.
+      const int last = __builtin_amdgcn_readfirstlane(end), begin = __builtin_amdgcn_readfirstlane(t0);
+      const int u = wave * NU / PA_WAVES;        // the group of 16 tokens it brings some of
+      const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_mem;
+      auto page_of = [&](int x) { return scalar_load(table, (min(x, last - 1) * T + 16 * u) >> D.page_shift); };
+      auto fetch = [&](int x, int page) __attribute__((always_inline)) {
+        const char *kb = row(kh, page, x * T + 16 * u), *vb = row(vh, page, x * T + 16 * u);
+        const uint32_t to = ring + (x - begin) % STAGES * STAGE_BYTES;
+        constexpr int PER = Ops::VW / 4;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int piece = 2 * wave + e;
+          to_lds(kb, k_off + piece % Ops::NK * 64, to + piece * 1024);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int piece = 2 * wave + e;
+          to_lds(vb, v_off + piece / PER % 4 * tok_bytes + piece % PER * 256, to + STAGE_BYTES / 2 + piece * 1024);
+        }
+      };
+      if (begin < last) {
+        __syncthreads();                         // (the problem before has been read)
+        int page[STAGES];
+#pragma unroll
+        for (int i = 0; i < STAGES; ++i) page[i] = page_of(begin + i);
+        look_up(begin, now);
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i)
+          if (begin + i < last) fetch(begin + i, page[i]);
+        int ahead = page[STAGES - 1];
+#pragma unroll
+        for (int i = 0; i < Ops::NK; ++i) asm volatile("" : "+v"(ops.q[i]));      // (here and not in the loop, which counts its loads itself)
+        for (int x = begin; x < last; ++x) {
+          if (x + STAGES - 1 < last) {
+            meet<4 * (STAGES - 2)>();            // tile x is there, and tile x - 1 has been read
+            fetch(x + STAGES - 1, ahead);
+          } else {
+            meet<0>();
+          }
+          ahead = page_of(x + STAGES);
+          look_up(min(x + 1, last - 1), next);
+          if (pair0 < pairs) tile(x, small_c, std::false_type{}, s_mem + (x - begin) % STAGES * STAGE_BYTES);
+          now = next;
+        }
+      }
+      if (t < t1) t = last;
+      if (t < t0) t = t0;
+    } else if (t < end) {
       look_up(t, now);
       look_up(min(t + STEP, nt - 1), next);
       load_k(t, now, small_c);
