@@ -162,6 +162,50 @@ def test_scores_of_any_size(gpu_device, dtype):
     assert (got[3] == 0).all() and np.isneginf(got_lse[3]).all()
 
 
+# 80 pairs of query row and head: a block of 64, whose wavefronts share tiles, and one of 16, of whose wavefronts one has pairs
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", [list(range(0, 330, 11)), [37 * i % 200 for i in range(300)], [5000, 3, 2000, 1]])
+def test_many_pairs_over_few_and_many_tiles(gpu_device, dtype, lens):
+    c = Case(gpu_device, lens, dtype=dtype, hq=32, rows=5)
+    lse = c.new_lse()
+    out = c.cache.step(*c.args(), c.on(c.k_new), c.on(c.v_new), c.on(c.q), lse=lse, decay=0.5)
+    c.oracle_append()
+    c.check_attend(out, lse, *c.oracle_attend(0.5))
+    c.check_weight()
+    c.check_pools()
+    assert c.cache.sync_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_pairs_and_pages_outside_the_pool(gpu_device, dtype):
+    c = Case(gpu_device, [700, 401, 90], dtype=dtype, hq=32, rows=5, weights=False)
+    for s, p, bad in ((0, 3, -1), (0, 4, 1 << 20), (0, 20, -7), (1, 0, 1 << 30), (1, 11, -1)):
+        c.d_table[s, p], c.table[s, p] = bad, bad
+    lse = c.new_lse()
+    out = c.cache.attend(*c.args(False), c.on(c.q), lse=lse)
+    c.check_attend(out, lse, *c.oracle_attend())
+    assert c.cache.sync_status() == -1 and c.cache.sync_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_pairs_are_not_touched_by_tokens_they_do_not_see(gpu_device, dtype):
+    c = Case(gpu_device, [333, 40, 32, 900], dtype=dtype, hq=32, rows=5)
+    for s, n in enumerate(c.lens):
+        p, i = c.table[s][(n - 1) // c.page], (n - 1) % c.page
+        c.v[p, 0, i, ::3], c.v[p, 1, i, ::5], c.k[p, 1, i, 7] = np.inf, np.nan, np.nan
+    c.cache.k_pages.copy_(c.on(c.k))
+    c.cache.v_pages.copy_(c.on(c.v))
+    lse = c.new_lse()
+    out = c.cache.attend(*c.args(False), c.on(c.q), lse=lse).double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want, want_lse = c.oracle_attend()
+    t = c.tolerances()
+    assert (np.abs(out[:, :4] - want[:, :4]) <= t["out_abs"] + 1.01 * t["out_rel"] * np.abs(want[:, :4])).all()
+    assert (np.abs(lse.cpu().numpy()[:, :4] - want_lse[:, :4]) <= t["lse"]).all()
+    assert not np.isfinite(out[:, 4, :16, ::3]).any() and np.isnan(out[:, 4, 16:]).all()
+
+
 def test_pool_beyond_32_bit_offsets(gpu_device):
     """Pages whose rows lie past 2^32 elements."""
     n_pages, page, hkv, d, T = 70000, 64, 8, 128, 5 * 64 + 9
