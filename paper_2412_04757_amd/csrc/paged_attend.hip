@@ -317,7 +317,7 @@ __device__ __forceinline__ void write_result(const PagedCall& a, size_t r, int c
 // cache (two or four blocks to a wavefront need more registers than there are: 16 rows of 4 heads over 32K tokens 80 us, this 55).
 // SHARED: four blocks of 128 columns read each tile from LDS, where all four wavefronts have brought it, three tiles ahead: 96 KB on
 // their way a compute unit instead of 32, a quarter of the requests. The same 40.5 us with its merge, without 58; one workgroup a compute
-// unit 43.8. 64 rows 98: a tile's 40 products and the exponentials of 64 pairs take the compute unit 0.66 us, its bytes 0.6.
+// unit 43.8. 64 rows 98: a tile's 24 products a wavefront and the exponentials of 64 pairs take the compute unit 0.66 us, its bytes 0.7.
 // SMALL: pages of fewer than 16 tokens, whose page is looked up lane by lane; else a group of 16 tokens lies in one page.
 template <int DT, int DIM, int WB, bool SMALL>
 __global__ __launch_bounds__(64 * PA_WAVES, 2) void paged_attend_kernel(PagedCall a, int min_share, int merge_later) {
