@@ -47,6 +47,8 @@ class LtriPagedCache:
                 if tuple(t.shape) != shape or t.dtype != self.tdtype or t.stride(3) != 1:
                     raise ValueError(f"pools are {self.tdtype} {shape} with dense rows; got {t.dtype} {tuple(t.shape)}, "
                                      f"strides {tuple(t.stride())}")
+            if any(n > 1 and step == 0 for n, step in zip(shape, k_pages.stride())):     # (three zeros would say "dense" to the library)
+                raise ValueError(f"pools whose rows overlap: strides {tuple(k_pages.stride())} of an expanded tensor")
             if k_pages.stride() != v_pages.stride():
                 raise ValueError(f"k_pages and v_pages differ in strides: {k_pages.stride()}, {v_pages.stride()}")
             cfg.page_stride, cfg.head_stride, cfg.token_stride = k_pages.stride()[:3]
