@@ -75,6 +75,7 @@ int32_t ltri_paged_create(const ltri_paged_config* cfg, void* k_pages, void* v_p
 /* Without device buffers: calls check their arguments and enqueue nothing. */
 int32_t ltri_paged_create_dry(const ltri_paged_config* cfg, ltri_paged** out);
 int32_t ltri_paged_destroy(ltri_paged* c);
+/* Stream of the following calls. Ordering it behind the old one's work, ltri_paged_create's included, is the caller's business (events). */
 int32_t ltri_paged_set_stream(ltri_paged* c, void* hip_stream);
 
 /* k_new, v_new: device [seq_count][n_kv_heads][n_new][head_dim]. Row i of sequence s goes to place lens[s] - n_new + i

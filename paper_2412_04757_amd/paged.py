@@ -27,7 +27,9 @@ class LtriPagedCache:
     k_pages, v_pages: [n_pages][n_kv_heads][page_tokens][head_dim], views of another order of the first three included
     (allocated here, zeroed, if not given); weight (fp32), pos (int32): [n_pages][n_kv_heads][page_tokens], with weights = 1.
     scratch: a uint8 tensor of at least scratch_bytes that caches whose calls do not overlap may share.
-    Work goes to the stream given here (default: the current one) or to set_stream()."""
+    Work goes to the stream given here (default: the current one) or to set_stream(); what is enqueued on other streams is the caller's
+    to order, and a call's tensors to keep until its work is done. The cache's own buffers may go at any time: the allocator is told of
+    every stream that used them. (A captured graph of its calls needs the cache as long as it is replayed.)"""
 
     def __init__(self, cfg: LtriPagedConfig, device: Optional[torch.device], dry: bool = False,
                  stream: Optional[torch.cuda.Stream] = None, k_pages: Optional[torch.Tensor] = None,
@@ -83,9 +85,16 @@ class LtriPagedCache:
             self.k_pages, self.v_pages, self.weight, self.pos = k_pages, v_pages, weight, pos
             self.state = torch.empty(self.state_bytes, dtype=torch.uint8, device=device)
             self.scratch = torch.empty(self.scratch_bytes, dtype=torch.uint8, device=device) if scratch is None else scratch
+            self._used_on(self.stream)
             self._check(self.lib.ltri_paged_create(C.byref(cfg), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(weight), _ptr(pos),
                                                    self.state.data_ptr(), _ptr(self.scratch), self.stream.cuda_stream,
                                                    C.byref(self.handle)))
+
+    def _used_on(self, stream: "torch.cuda.Stream") -> None:
+        """The buffers' memory is not given to others before the work that this stream has by then is done, wherever they were allocated."""
+        for t in (self.k_pages, self.v_pages, self.weight, self.pos, self.state, self.scratch):
+            if t is not None:
+                t.record_stream(stream)
 
     def _check(self, status: int) -> None:
         if status != 0:
@@ -136,8 +145,11 @@ class LtriPagedCache:
 
     # ---- the C ABI, same names ----
     def set_stream(self, stream: "torch.cuda.Stream") -> None:
-        if not self.dry and stream.device != self.device:
-            raise ValueError(f"a stream of {stream.device}, the cache is on {self.device}")
+        """ltri_paged_set_stream: the caller orders the new stream behind the old one's work (stream.wait_stream), creation included."""
+        if not self.dry:
+            if stream.device != self.device:
+                raise ValueError(f"a stream of {stream.device}, the cache is on {self.device}")
+            self._used_on(stream)
         self._check(self.lib.ltri_paged_set_stream(self.handle, stream.cuda_stream))
         self.stream = stream
 

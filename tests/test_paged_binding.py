@@ -1,4 +1,6 @@
-"""The binding of the paged cache without a GPU: which pools it takes."""
+"""The binding of the paged cache without a GPU: which pools it takes, and that the allocator hears of the streams."""
+from types import SimpleNamespace
+
 import pytest
 import torch
 
@@ -35,3 +37,19 @@ def test_pools_whose_rows_overlap_otherwise_are_refused():
         with pytest.raises(LtriError) as e:
             LtriPagedCache(config(5, 3, 8), None, dry=True, k_pages=pool, v_pages=pool)
         assert e.value.status == -1
+
+
+def test_the_allocator_is_told_of_every_stream():
+    """A buffer that only its stream of creation is known for could be given to others while the work of a later stream still uses it."""
+    cache = LtriPagedCache(config(5, 3, 8), None, dry=True)
+    names, heard = ("k_pages", "v_pages", "weight", "pos", "state", "scratch"), []
+    for name in names:
+        setattr(cache, name, SimpleNamespace(record_stream=lambda s, name=name: heard.append((name, s))))
+    cache.pos = None                                           # (a cache without positions)
+    cache.dry, cache.device = False, "here"
+    side = SimpleNamespace(device="here", cuda_stream=16)
+    cache.set_stream(side)
+    assert sorted(heard, key=lambda x: names.index(x[0])) == [(n, side) for n in names if n != "pos"] and cache.stream is side
+    with pytest.raises(ValueError):
+        cache.set_stream(SimpleNamespace(device="there", cuda_stream=32))
+    assert len(heard) == 5 and cache.stream is side
