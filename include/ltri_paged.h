@@ -32,8 +32,10 @@
  * the handle's stream without waiting. A call runs on the device that was current at creation, whatever is current when it is made. Calls on one
  * handle must not overlap; handles may share a scratch buffer if their calls do not overlap. k/v pages and rows, q and
  * out are 16-byte aligned (EINVAL else). What only the device can see is reported by ltri_paged_sync_status(): a length
- * beyond the table's capacity (LTRI_ECAPACITY; the sequence is taken as length 0) and a page outside [0, n_pages)
- * (LTRI_EINVAL; its tokens are not attended and not written, and its sequence is not evicted).
+ * beyond the table's capacity (LTRI_ECAPACITY; the sequence is taken as length 0), a page outside [0, n_pages)
+ * (LTRI_EINVAL; its tokens are not attended and not written, and its sequence is not evicted) and, where weights are written
+ * or tokens evicted, sequences that together hold more tokens than the pool, be it by a page named twice or by pages outside it
+ * (LTRI_ECAPACITY; the attention is whole, but sequences that found no room in scratch may keep their weights or stay unevicted).
  */
 #ifndef LTRI_PAGED_H
 #define LTRI_PAGED_H

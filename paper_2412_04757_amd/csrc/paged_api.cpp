@@ -311,6 +311,8 @@ int32_t ltri_paged_sync_status(ltri_paged* c) {
   if (r != LTRI_OK || e[0] == 0) return r;
   r = check_hip(c, launch_fill_zero(c->state + c->L.err, 16, c->stream), "clear the error word");
   if (r != LTRI_OK) return r;
+  if (e[0] == PAGED_NO_ROOM)
+    return fail(c, LTRI_ECAPACITY, "raised on the device: more tokens in a call than the pool holds (a page named twice?); weights or evictions are left out");
   return fail(c, e[0], "raised on the device: %s", e[0] == LTRI_ECAPACITY ? "a length beyond the page table"
                                                                           : "a page outside the pool");
 }

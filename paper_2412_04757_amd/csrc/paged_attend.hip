@@ -836,7 +836,7 @@ __global__ __launch_bounds__(WALK_T) void paged_weights_kernel(PagedCall a) {
     x += WALK_T / 64;
     const float* scores = score_rows(a, units, nt, TILE, h);
     if (!scores) {
-      if (lane == 0) atomicCAS(a.err, 0, LTRI_ECAPACITY);
+      if (lane == 0) atomicCAS(a.err, 0, PAGED_NO_ROOM);
       continue;
     }
     const int i0 = piece * PW_TOKENS + 4 * lane, at_most = nt * TILE - 4;

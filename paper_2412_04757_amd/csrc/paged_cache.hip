@@ -271,7 +271,7 @@ __global__ __launch_bounds__(EV_T) void paged_select_kernel(PagedCall a) {
     half = min(keep, n - keep);                   // both lists have `count` entries, at most this
     const long long before = list_tiles_before(a, s);
     if (before + paged_tiles(n) > D.score_tiles) {
-      if (tid == 0) atomicCAS(a.err, 0, LTRI_ECAPACITY);
+      if (tid == 0) atomicCAS(a.err, 0, PAGED_NO_ROOM);
       return;
     }
     to = a.moves + list_base(a, before, n, h);
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(EV_T) void paged_long_keys_kernel(PagedCall a) {
   pick_bin<0>(hist, &s_pick, prefix, rank, all);
   if (tid == 0) {
     const bool live = room && !__hip_atomic_load(state + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (!room) atomicCAS(a.err, 0, LTRI_ECAPACITY);
+    if (!room) atomicCAS(a.err, 0, PAGED_NO_ROOM);
     state[1] = 0;
     *L = LongSlot{(long long)base, prefix, rank, (int)all, (int)live};
     a.move_head[2 * slot + 1] = 0;

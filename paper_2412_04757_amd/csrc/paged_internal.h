@@ -25,6 +25,10 @@ constexpr int EV_LONG = 16384, EV_CHUNK = 4096;
 constexpr int EV_LONG_WORDS = 4 + 2048;    // counters of a (sequence, KV head), zero between launches
 constexpr int EV_SLOT_BYTES = 24;          // what the launches of a long selection tell each other
 
+// In the device's error word beside the statuses: a sequence whose scores or lists of moves find no room in scratch, which holds the
+// pool's tokens. Told as LTRI_ECAPACITY.
+constexpr int PAGED_NO_ROOM = 1;
+
 struct PagedDims {
   int Hq, Hkv, G, d, dtype, elt;
   int page_shift, n_pages, table_pages, max_seqs, rows_max, weights;
