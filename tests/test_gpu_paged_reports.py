@@ -58,3 +58,16 @@ def test_more_tokens_than_the_pool_holds(gpu_device):
     t = c.tolerances()["weight"] + 4 * 2.0 ** -23                  # (as in Case.check_weight)
     assert (np.abs(cache.weight.double().cpu().numpy() - weight) <= t * np.abs(weight) + 2.0 ** -30).all()
     assert cache.sync_status() == 0
+
+
+@pytest.mark.parametrize("seqs,status", [(1, 0), (2, -3), (12, -3)])
+def test_pages_named_twice_with_weights_touch_nothing_else(gpu_device, seqs, status):
+    """Which weights such a call leaves is not defined; rows and positions stay, and nothing is written behind the scratch."""
+    c, plain, table, lens = crowded(gpu_device, seqs)
+    guard = 1 << 20
+    scratch = torch.full((plain.scratch_bytes + guard,), 0xFF, dtype=torch.uint8, device=gpu_device)
+    cache = LtriPagedCache(plain.cfg, gpu_device, k_pages=plain.k_pages, v_pages=plain.v_pages, weight=plain.weight, pos=plain.pos, scratch=scratch)
+    before = [x.clone() for x in (cache.k_pages, cache.v_pages, cache.pos)]
+    cache.attend(table, lens, c.on(c.q).repeat(seqs, 1, 1, 1), decay=1.0)
+    assert all(same(x, y) for x, y in zip(before, (cache.k_pages, cache.v_pages, cache.pos)))
+    assert bool((scratch[plain.scratch_bytes:] == 0xFF).all()) and cache.sync_status() == status
