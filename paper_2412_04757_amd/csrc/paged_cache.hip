@@ -107,33 +107,24 @@ __device__ __forceinline__ void pick_bin(const int* hist, Picked* s_pick, uint32
 // The keys of PER tokens at first, first + stride, ..., below n (others: 0): places, then marks, all on their way together (one
 // after the other ten tokens took 8.7 us, so 2.9). bad: a page is not in the pool.
 template <int PER>
-__device__ __forceinline__ void load_keys(const PagedCall& a, int s, int h, int n, int first, int stride, int count,
-                                          uint32_t (&key)[PER], bool& bad) {
+__device__ __forceinline__ void load_keys(const PagedCall& a, int s, int h, int n, int first, int stride, uint32_t (&key)[PER], bool& bad) {
   const PagedDims& D = a.D;
   const int32_t* table = a.table + (size_t)s * D.table_pages;
   const int seen = a.seen[s];
-  constexpr int AT_ONCE = PER < 16 ? PER : 16;
+  int page[PER], pos[PER];
+  float w[PER];
 #pragma unroll
-  for (int e0 = 0; e0 < PER; e0 += AT_ONCE) {
+  for (int e = 0; e < PER; ++e) page[e] = table[min(first + e * stride, n - 1) >> D.page_shift];
 #pragma unroll
-    for (int e = 0; e < AT_ONCE; ++e) key[e0 + e] = 0u;
-    if (e0 >= count) continue;                     // (uniform)
-    int page[AT_ONCE], pos[AT_ONCE];
-    float w[AT_ONCE];
-#pragma unroll
-    for (int e = 0; e < AT_ONCE; ++e) page[e] = table[min(first + (e0 + e) * stride, n - 1) >> D.page_shift];
-#pragma unroll
-    for (int e = 0; e < AT_ONCE; ++e) {
-      const bool good = (unsigned)page[e] < (unsigned)D.n_pages;
-      bad |= !good;
-      const size_t mark = paged_mark(D, good ? page[e] : 0, h, min(first + (e0 + e) * stride, n - 1));
-      pos[e] = a.pos[mark];
-      w[e] = a.weight[mark];
-    }
-#pragma unroll
-    for (int e = 0; e < AT_ONCE; ++e)
-      if (first + (e0 + e) * stride < n) key[e0 + e] = evict_key(a, pos[e], w[e], seen);
+  for (int e = 0; e < PER; ++e) {
+    const bool good = (unsigned)page[e] < (unsigned)D.n_pages;
+    bad |= !good;
+    const size_t mark = paged_mark(D, good ? page[e] : 0, h, min(first + e * stride, n - 1));
+    pos[e] = a.pos[mark];
+    w[e] = a.weight[mark];
   }
+#pragma unroll
+  for (int e = 0; e < PER; ++e) key[e] = first + e * stride < n ? evict_key(a, pos[e], w[e], seen) : 0u;
 }
 
 // Tiles of scratch in front of a sequence (each (sequence, KV head) has PAGED_TILE entries a tile); every wavefront adds for itself.
@@ -205,7 +196,7 @@ __global__ __launch_bounds__(EV_T) void paged_select_kernel(PagedCall a) {
   const int per = (n + EV_T - 1) / EV_T, base = wave * 64 * per + lane;
   uint32_t key[PER];
   bool bad = false;
-  load_keys(a, s, h, n, base, 64, per, key, bad);
+  load_keys(a, s, h, n, base, 64, key, bad);
   __syncthreads();
   if (bad) s_bad = 1;
   uint32_t prefix = 0u;
@@ -362,10 +353,10 @@ __global__ __launch_bounds__(EV_T) void paged_long_keys_kernel(PagedCall a) {
   const long long before = list_tiles_before(a, s);
   const bool room = before + paged_tiles(n) <= D.score_tiles;
   const size_t base = list_base(a, before, n, h);
-  int32_t* state = a.long_state + (size_t)slot * EV_LONG_WORDS;         // [0] ticket, [1] bad pages, [2] candidates, [3] unused, then the histogram
+  int32_t* state = a.long_state + (size_t)slot * EV_LONG_WORDS;         // [0] ticket, [1] bad pages, [2] candidates, from [4] on the histogram
   bool bad = false;
   uint32_t key[EV_CHUNK / EV_T];
-  load_keys(a, s, h, n, first + tid, EV_T, EV_CHUNK / EV_T, key, bad);
+  load_keys(a, s, h, n, first + tid, EV_T, key, bad);
   __syncthreads();
 #pragma unroll
   for (int e = 0; e < EV_CHUNK / EV_T; ++e) {
