@@ -67,8 +67,9 @@ typedef struct {
 } ltri_paged_config;
 
 /* Bytes of the two device buffers of a handle: `state` (counters, the device's error word; as long as the handle
- * lives; ltri_paged_create enqueues a kernel that clears it) and `scratch` (temporaries of a call: partial results,
- * with weights also scores and lists of moves, which grow with the pool). EINVAL on an unsupported configuration. */
+ * lives; ltri_paged_create enqueues a kernel that clears it) and `scratch` (temporaries of a call: partial results;
+ * with weights also lists of moves, 4 to 12 bytes, and scores, 4 min(rows_max n_q_heads / n_kv_heads, 31) bytes, for every token of the pool and
+ * KV head: 8 KV heads of 4, a pool of 1M tokens, rows_max 1: 151 MB, 7: 974 MB). EINVAL on an unsupported configuration. */
 int32_t ltri_paged_workspace_bytes(const ltri_paged_config* cfg, size_t* state_bytes, size_t* scratch_bytes);
 
 /* All pointers are device memory of the current device and the caller's; state and scratch 256-byte aligned. */

@@ -93,8 +93,9 @@ __device__ __forceinline__ float second_float(unsigned long long v) { return __u
 __device__ __forceinline__ float safe_ref(float m) { return m == -INFINITY ? 0.f : m; }
 
 // A wavefront's matrix products of one tile, by type. NU: groups of 16 tokens in a tile; VW: 32-bit words of a lane's piece of a value row.
-// ONCE: no other wavefront reads these rows: they pass the caches by. 16 x 128K tokens 1394 -> 1268 us, 64 ragged sequences
-// 193 -> 180; where wavefronts share rows (16 query rows over 32K) it is 59 -> 85.
+// ONCE: no other wavefront of the problem reads these rows: they pass the caches by. 16 x 128K tokens 1394 -> 1268 us, 64 ragged sequences
+// 193 -> 180; where wavefronts share rows (16 query rows over 32K) it is 59 -> 85. It knows nothing of pages that sequences share: 64 of 8704
+// tokens, 8192 of them the same pages, take 201 us with it and 159 without, with pages of their own 340 and 382.
 template <bool ONCE, class T> __device__ __forceinline__ T load_row(const char* p) {
   if constexpr (ONCE) return __builtin_nontemporal_load((const T*)p);
   else return *(const T*)p;
@@ -872,7 +873,8 @@ __global__ __launch_bounds__(WALK_T) void paged_weights_kernel(PagedCall a) {
 
 // The same from the keys, for many pairs (see paged_keeps_scores): the scores again, one tile of keys after the other, with the
 // log-sum-exps at hand. The queries of 64 pairs stay in registers; the next tile's keys are on their way while one is used.
-// 64 pairs over 32K tokens, 8 KV heads: 18 us for 67 MB of keys.
+// 64 pairs over 32K tokens, 8 KV heads: 18 us for 67 MB of keys. More pairs go over the keys again for every 64, and over the weights:
+// 512 pairs over 32K tokens, one KV head: 35 us (28 with loads that stay in the caches), 2048 pairs 122 (94).
 template <int DT, int DIM>
 __global__ __launch_bounds__(WALK_T, 2) void paged_key_weights_kernel(PagedCall a) {
   constexpr int T = PagedTile<DT>::N, ELT = DT == LTRI_F32 ? 4 : 2, WAVES = WALK_T / 64, NB = 4;
@@ -1007,7 +1009,8 @@ static void launch_key_weights(const PagedCall& a, int wgs, hipStream_t s) {
 
 // A launch of its own for the merge from this many bytes of a problem's partial results on. One sequence, 8 KV heads of 4: 128K
 // tokens (131 KB) 107.5 us with the last workgroup, 104.9 with the launch; 32K tokens of 16 rows (2 MB) 147 and 60; fp32, 2 x 4097
-// tokens of one KV head, 64 wide (66 KB) 12.7 and 15.3.
+// tokens of one KV head, 64 wide (66 KB) 12.7 and 15.3. The host does not know the lengths: a long sequence among empty or short ones is
+// merged by the last workgroup (16 rows over 32K tokens alone 40 us, beside 63 empty sequences 124, beside 63 of 100 tokens 97).
 constexpr long long MERGE_BYTES = 96 << 10;
 
 hipError_t launch_paged_attend(const PagedCall& a, hipStream_t s) {

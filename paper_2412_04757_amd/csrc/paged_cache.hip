@@ -578,6 +578,9 @@ static void launch_select(const PagedCall& a, hipStream_t s) {
   else paged_select_kernel<EV_LONG / EV_T, FEW><<<grid, EV_T, 0, s>>>(a);
 }
 
+// Which way goes by what the table could hold, as the host does not know the lengths: 16 sequences of 5125 tokens, one of which goes, take
+// 14 us with a table of 5184 tokens (one launch), 18 with 8192 (two), 54 with 32768 (five) and 138 with 131072 (five, of whose workgroups
+// most find nothing).
 hipError_t launch_paged_evict(const PagedCall& a, hipStream_t s) {
   const PagedDims& D = a.D;
   const long long most = std::min<long long>(a.keep, D.cap_tokens - a.keep);      // moves of a sequence and KV head

@@ -20,7 +20,7 @@ __host__ __device__ constexpr bool paged_keeps_scores(int pairs) { return pairs 
 
 // Eviction: tables of up to EV_LONG tokens are selected from by one workgroup per (sequence, KV head), longer ones by several, EV_CHUNK
 // tokens each. One sequence of 8 KV heads, us with its append of 2K: one workgroup 16K tokens 43, 22K 52, 32K 60; several 22K tokens
-// 46, 32K 46.
+// 46, 32K 46. (The rule looks at the table alone: with more sequences one workgroup each fills more of the chip.)
 constexpr int EV_LONG = 16384, EV_CHUNK = 4096;
 constexpr int EV_LONG_WORDS = 4 + 2048;    // counters of a (sequence, KV head), zero between launches
 constexpr int EV_SLOT_BYTES = 24;          // what the launches of a long selection tell each other
