@@ -1,7 +1,8 @@
-"""Buffers of the paged cache on other streams than those they were allocated on."""
+"""The paged cache on other streams than those its buffers were allocated on, and in captured graphs."""
 import pytest
 import torch
 
+from oracle import paged_oracle as O
 from paged_util import Case
 from paper_2412_04757_amd import LtriPagedCache
 
@@ -38,3 +39,82 @@ def test_a_dropped_cache_keeps_its_memory_until_its_stream_is_done(gpu_device, g
             assert all(x.data_ptr() + x.numel() <= p or p + n <= x.data_ptr() for p, n in mine.items())
     torch.cuda.synchronize()
     c.check_attend(out, None, *c.oracle_attend())
+
+
+def bits(x):
+    return torch.nan_to_num(x.float(), nan=-5.0)
+
+
+@pytest.mark.parametrize("dtype,page,tokens,rows,keep", [
+    ("bf16", 16, 700, 5, 320), ("f32", 16, 700, 5, 320),          # tiles through LDS, the keys again for the weights, lists and moves
+    ("bf16", 8, 300, 2, 290),                                     # small pages, the eviction in one launch
+    ("bf16", 64, 18000, 16, 9000),                                # a merge launch, an eviction by several workgroups
+])
+def test_captured_calls_of_every_way(gpu_device, dtype, page, tokens, rows, keep):
+    """The stream is set inside the capture; every replay, with eager work of another cache in between, is the eager call's to the bit."""
+    a = Case(gpu_device, [tokens, 40, 0, tokens // 2], dtype=dtype, hq=32, hkv=2, page=page, rows=rows, room=8 * rows, seed=3)
+    twin = LtriPagedCache(a.cache.cfg, gpu_device, k_pages=a.cache.k_pages.clone(), v_pages=a.cache.v_pages.clone(), weight=a.cache.weight.clone(),
+                          pos=a.cache.pos.clone())
+    table, lens, seen = a.d_table, a.d_lens.clone(), a.d_seen.clone()
+    k, v, q = a.on(a.k_new), a.on(a.v_new), a.on(a.q)
+    out, lse = torch.empty_like(q), a.new_lse()
+
+    def body(cache, n):
+        cache.step(table, n, seen, k, v, q, out=out, lse=lse, decay=0.9)
+        cache.evict(table, n, seen, keep, n_sink=4, n_recent=20)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        twin.set_stream(torch.cuda.current_stream())
+        body(twin, lens)
+    for _ in range(5):
+        for x in (k, v, q):
+            x.copy_(a.on(a.values(x.shape)))
+        seen += rows * (lens > 0).int()
+        lens += rows * (lens > 0).int()
+        eager = lens.clone()
+        body(a.cache, eager)
+        want = [out.clone(), lse.clone()]
+        out.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1]) and torch.equal(lens, eager)
+        for x, y in ((twin.k_pages, a.cache.k_pages), (twin.v_pages, a.cache.v_pages), (twin.weight, a.cache.weight), (twin.pos, a.cache.pos)):
+            assert torch.equal(bits(x), bits(y))
+    assert int(lens.max()) == keep and a.cache.sync_status() == 0
+    twin.set_stream(torch.cuda.current_stream())
+    assert twin.sync_status() == 0
+
+
+@pytest.mark.parametrize("lens,page,keep", [([300, 120, 0], 16, 200), ([1500, 900], 16, 700), ([17000, 12000], 128, 9000)])
+def test_lengths_that_are_also_the_tokens_seen(gpu_device, lens, page, keep):
+    """One array for both, as before anything was ever evicted; the call writes it."""
+    c = Case(gpu_device, lens, hq=2, hkv=2, dim=64, page=page)
+    both = c.d_lens
+    c.cache.evict(c.d_table, both, both, keep, n_sink=4, n_recent=50)
+    O.evict(c.k, c.v, c.weight, c.pos, c.table, c.lens, c.seen, keep, 4, 50)
+    assert both.tolist() == c.lens.tolist()
+    c.check_pools()
+    assert c.cache.sync_status() == 0
+
+
+def test_two_caches_on_two_streams_at_once(gpu_device):
+    """Buffers of their own, the calls of both under way together."""
+    cases = [Case(gpu_device, [3000, 41, 0, 800], hq=32, rows=5, seed=7 + i) for i in range(2)]
+    streams, got = [torch.cuda.Stream(gpu_device) for _ in cases], []
+    inputs = [(c.on(c.k_new), c.on(c.v_new), c.on(c.q), c.new_lse()) for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = []
+        for c, s, (k, v, q, lse) in zip(cases, streams, inputs):
+            c.cache.set_stream(s)
+            got.append(c.cache.step(*c.args(), k, v, q, lse=lse, decay=0.0))
+    torch.cuda.synchronize()
+    for c, out, (_, _, _, lse) in zip(cases, got, inputs):
+        c.oracle_append()
+        c.check_attend(out, lse, *c.oracle_attend(0.0))
+        c.check_weight()
+        c.check_pools()
+        assert c.cache.sync_status() == 0
